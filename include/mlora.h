@@ -324,6 +324,78 @@ int mlora_attention(const void* q, const void* prefix_k, const void* prefix_v, i
                     int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, void* out, void* workspace,
                     size_t workspace_bytes, int32_t* status, void* cuda_stream);
 
+/* ---- operators around a bounded KV cache (kernel-level) ----
+ * What a program that drives the kernel-level calls itself needs between its projections and mlora_attention, and what lets a
+ * stream run on when its own segment is full: rotate and append a pass's rows, attend while totalling what every cached key
+ * contributes, drop the keys that contribute least.  own_weight and own_position lie beside the own segments, one entry for
+ * every row of every KV head: float / int32 [n_streams][n_kv_heads][own_capacity].  The own segment is a set as far as
+ * attention goes (a key's position is in its rotation), so rows may lie in any order.  head_dim 64 or 128; K, V, q and out
+ * 16-byte aligned.  All pointers are of the current device.  Lengths that only the device sees and that are out of range set
+ * the status word; the call then stays in bounds.  A workspace serves one call at a time. */
+
+/* Frequencies of rotary positions: freq (host double [rotary_dim / 2]) receives radians per position of each pair, *gain
+ * (host) the factor on cos and sin.  PLAIN: f_i = theta^(-2 i / rotary_dim).  For contexts longer than a model was trained on
+ * (factor >= 1 times `length` positions): LINEAR: f_i / factor.  BASE: theta * factor^(d / (d - 2)).  WAVES: pairs that turn
+ * at most `low` times in `length` positions are divided by factor, those that turn `high` times and more stay, a linear blend by
+ * turns between.  RAMP ("YaRN"): the same two ends, a linear blend by pair index between them (floor / ceil of the pairs that
+ * turn `high` / `low` times), gain 0.1 ln(factor) + 1.  Unused arguments are ignored.  Host only.  Errors: ARG. */
+enum { MLORA_ROPE_PLAIN = 0, MLORA_ROPE_LINEAR = 1, MLORA_ROPE_BASE = 2, MLORA_ROPE_WAVES = 3, MLORA_ROPE_RAMP = 4 };
+int mlora_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, double length, double low,
+                           double high, double* freq, float* gain);
+/* Rotates the query and key rows of a pass and appends its K/V rows to the own segments (Sec. 3.1).  Row r = stream * n_nodes
+ * + node has position positions[r] (dev int32, any value); its K/V row becomes row suffix_len[stream] + node of the stream's own segment.
+ * q [rows][n_q_heads][head_dim], k, v [rows][n_kv_heads][head_dim]: dev fp16 (in_fp32 = 0) or fp32 (1: as mlora_linear writes
+ * them), rows `*_stride` elements apart (a multiple of 16 bytes), heads packed.  The first rotary_dim features of a head (a
+ * multiple of 16) turn in pairs (i, i + rotary_dim / 2) (interleaved = 0) or (2 i, 2 i + 1) (1), the others and v pass through.
+ * freq: dev double [rotary_dim / 2], gain: see mlora_rope_frequencies.  q_out dev fp16 [rows][n_q_heads][head_dim]; it may be q
+ * itself where q is fp16 and packed.  own_weight, own_position (NULL: not kept): the new rows' entries become 0 and
+ * positions[r].  q and q_out NULL: append only.  k, v, own_k, own_v NULL: rotate q only (n_streams * n_nodes rows,
+ * suffix_len and status not read).  suffix_len is not changed.  n_nodes has no limit here: with n_streams = 1 and
+ * own_capacity = prefix_len this fills a shared prefix.
+ * Errors: ARG, UNSUPPORTED, CAPACITY (n_nodes > own_capacity), CUDA; a stream whose rows do not fit behind suffix_len[stream]
+ * appends nothing and sets the device status to MLORA_ERR_CAPACITY. */
+int mlora_rope_append(const void* q, const void* k, const void* v, int32_t in_fp32, int64_t q_stride, int64_t k_stride,
+                      int64_t v_stride, const int32_t* positions, const double* freq, float gain, int32_t rotary_dim,
+                      int32_t interleaved, int32_t n_streams, int32_t n_nodes, int32_t n_q_heads, int32_t n_kv_heads,
+                      int32_t head_dim, void* q_out, void* own_k, void* own_v, int32_t own_capacity, const int32_t* suffix_len,
+                      float* own_weight, int32_t* own_position, int32_t* status, void* cuda_stream);
+
+/* Bytes of scratch for mlora_attention_scored with this suffix_bound or any smaller one. */
+size_t mlora_attention_scored_workspace_bytes(int32_t n_streams, int32_t n_nodes, int32_t n_q_heads, int32_t n_kv_heads,
+                                              int32_t head_dim, int32_t prefix_len, int32_t suffix_bound);
+/* mlora_attention (same tensors, layouts and mask) that also totals softmax weights: own_weight[s][h][j] grows by the sum, over
+ * the stream's n_nodes rows and the query heads that share KV head h, of the weight they give row j of the own segment (cached
+ * rows and the pass's own); prefix_weight dev fp32 [n_kv_heads][prefix_len] (NULL: not wanted) by the same sum over the rows of
+ * all streams.  Entries of rows behind suffix_len + n_nodes are not touched.  tree_parent may be NULL: the pass's rows form a
+ * chain.  n_nodes <= 64.  The rows of a pass should be finite: a weight of zero times an infinite or NaN value is NaN.  Results do
+ * not depend on the order in which the GPU runs the work.
+ * Errors: ARG, UNSUPPORTED, CAPACITY (suffix_bound + n_nodes > own_capacity, workspace), CUDA; a malformed parent array or a
+ * suffix_len outside 0..suffix_bound sets the device status to MLORA_ERR_ARG. */
+int mlora_attention_scored(const void* q, const void* prefix_k, const void* prefix_v, int32_t prefix_len,
+                           const void* own_k, const void* own_v, int32_t own_capacity, const int32_t* suffix_len,
+                           int32_t suffix_bound, const int32_t* tree_parent, int32_t n_streams, int32_t n_nodes,
+                           int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, void* out, float* own_weight,
+                           float* prefix_weight, void* workspace, size_t workspace_bytes, int32_t* status, void* cuda_stream);
+
+/* Bytes of scratch for mlora_kv_evict with this suffix_bound or any smaller one. */
+size_t mlora_kv_evict_workspace_bytes(int32_t n_streams, int32_t n_kv_heads, int32_t suffix_bound, int32_t budget);
+/* Cuts every own segment that is longer to `budget` rows, for each KV head on its own.  Of the rows 0 .. suffix_len[s] - 1 the
+ * first `budget` stay in the order: rows whose position exceeds newest[s] - recent (recent = 0: none; newest dev int32
+ * [n_streams]), then falling own_weight (NaN lowest, -0 equals +0), then rising index.  Rows that stay and lie below index
+ * `budget` stay where they are; the others that stay move, in rising order, to the places of the dropped rows, in rising
+ * order.  Their own_weight and own_position go with them: entries 0 .. out_len[s] - 1 of out_weight and out_position are
+ * written for all rows that are left.  out_weight may be own_weight and out_position own_position; own_position and out_position may both
+ * be NULL where recent is 0.  out_len dev int32 [n_streams] = min(suffix_len, budget), never suffix_len itself.
+ * out_source dev int32 [n_streams][n_kv_heads][budget] or NULL: the index that each row had before.
+ * Rows and entries from index out_len[s] on are left as they were.
+ * Errors: ARG (recent > budget, ...), UNSUPPORTED, CAPACITY (suffix_bound > own_capacity, workspace), CUDA; a suffix_len
+ * outside 0..suffix_bound sets the device status to MLORA_ERR_ARG. */
+int mlora_kv_evict(void* own_k, void* own_v, const float* own_weight, const int32_t* own_position, int32_t own_capacity,
+                   const int32_t* suffix_len, int32_t suffix_bound, const int32_t* newest, int32_t budget, int32_t recent,
+                   int32_t n_streams, int32_t n_kv_heads, int32_t head_dim, float* out_weight, int32_t* out_position,
+                   int32_t* out_len, int32_t* out_source, void* workspace, size_t workspace_bytes, int32_t* status,
+                   void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

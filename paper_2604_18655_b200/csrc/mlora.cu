@@ -4,12 +4,14 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <unordered_map>
 #include <vector>
 
 #include "../../include/mlora.h"
+#include "cache_ops.cuh"
 #include "common.cuh"
 
 using namespace mlora;
@@ -1966,6 +1968,174 @@ int mlora_attention(const void* q, const void* prefix_k, const void* prefix_v, i
   a.part_ml = a.part_o + (attn_workspace_floats(a) / (hd + 2)) * hd;
   CK(launch_attention(a, st));
   CK(launch_attention_merge(a, st));
+  return MLORA_OK;
+}
+
+// ----------------------------------------------------------------------------- operators around a bounded KV cache
+int mlora_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, double length, double low, double high,
+                           double* freq, float* gain) {
+  if (!freq || !gain) return fail(MLORA_ERR_ARG, "null argument");
+  if (rotary_dim < 2 || rotary_dim % 2 || !(theta > 1.0) || !std::isfinite(theta)) return fail(MLORA_ERR_ARG, "rotary_dim must be even and positive, theta above 1");
+  if (scaling < MLORA_ROPE_PLAIN || scaling > MLORA_ROPE_RAMP) return fail(MLORA_ERR_ARG, "unknown scaling");
+  if (scaling != MLORA_ROPE_PLAIN && !(factor >= 1.0 && std::isfinite(factor))) return fail(MLORA_ERR_ARG, "factor must be at least 1");
+  if (scaling >= MLORA_ROPE_WAVES && !(length > 0.0 && low > 0.0 && high > low && std::isfinite(length) && std::isfinite(high)))
+    return fail(MLORA_ERR_ARG, "needs length > 0 and 0 < low < high");
+  const double two_pi = 6.283185307179586476925;
+  const int m = rotary_dim / 2;
+  if (scaling == MLORA_ROPE_BASE && rotary_dim > 2) theta *= std::pow(factor, rotary_dim / (rotary_dim - 2.0));
+  double r0 = 0.0, r1 = 1.0;                               // ramp: from pair r0 (as it is) to pair r1 (divided)
+  if (scaling == MLORA_ROPE_RAMP) {
+    auto pair_of = [&](double turns) { return rotary_dim * std::log(length / (turns * two_pi)) / (2.0 * std::log(theta)); };
+    r0 = std::fmax(std::floor(pair_of(high)), 0.0);
+    r1 = std::fmin(std::ceil(pair_of(low)), rotary_dim - 1.0);
+    if (r1 - r0 < 1e-3) r1 = r0 + 1e-3;
+  }
+  for (int i = 0; i < m; ++i) {
+    double f = std::pow(theta, -2.0 * i / rotary_dim);
+    if (scaling == MLORA_ROPE_LINEAR) f /= factor;
+    if (scaling == MLORA_ROPE_WAVES) {
+      const double w = std::fmin(std::fmax((length * f / two_pi - low) / (high - low), 0.0), 1.0);
+      f = (1.0 - w) * f / factor + w * f;
+    }
+    if (scaling == MLORA_ROPE_RAMP) {
+      const double w = std::fmin(std::fmax((i - r0) / (r1 - r0), 0.0), 1.0);
+      f = w * f / factor + (1.0 - w) * f;
+    }
+    freq[i] = f;
+  }
+  *gain = scaling == MLORA_ROPE_RAMP ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
+  return MLORA_OK;
+}
+
+static bool misaligned16(std::initializer_list<const void*> ptrs) {
+  uintptr_t bits = 0;
+  for (const void* p : ptrs) bits |= (uintptr_t)p;
+  return (bits & 15) != 0;
+}
+
+int mlora_rope_append(const void* q, const void* k, const void* v, int32_t in_fp32, int64_t q_stride, int64_t k_stride,
+                      int64_t v_stride, const int32_t* positions, const double* freq, float gain, int32_t rotary_dim,
+                      int32_t interleaved, int32_t n, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, void* q_out, void* own_k,
+                      void* own_v, int32_t own_capacity, const int32_t* suffix_len, float* own_weight, int32_t* own_position,
+                      int32_t* status, void* cuda_stream) {
+  const bool app = own_k != nullptr;
+  if (!positions || !freq) return fail(MLORA_ERR_ARG, "rope_append: null argument");
+  if ((q == nullptr) != (q_out == nullptr)) return fail(MLORA_ERR_ARG, "rope_append: q and q_out go together");
+  if ((k == nullptr) == app || (v == nullptr) == app || (own_v == nullptr) == app)
+    return fail(MLORA_ERR_ARG, "rope_append: k, v, own_k and own_v go together");
+  if (!q && !app) return fail(MLORA_ERR_ARG, "rope_append: nothing to do");
+  if (app && (!suffix_len || !status)) return fail(MLORA_ERR_ARG, "rope_append: null suffix_len or status");
+  if (!app && (own_weight || own_position)) return fail(MLORA_ERR_ARG, "rope_append: own_weight and own_position belong to appended rows");
+  if (n <= 0 || T <= 0 || (q && Hq <= 0) || (app && Hkv <= 0) || (long long)n * T > (1 << 28) || Hq < 0 || Hkv < 0 || Hq + 2ll * Hkv > (1 << 16))
+    return fail(MLORA_ERR_ARG, "rope_append: bad shape");
+  if (hd != 64 && hd != 128) return fail(MLORA_ERR_UNSUPPORTED, "rope_append: head_dim must be 64 or 128");
+  if (rotary_dim < 16 || rotary_dim > hd || rotary_dim % 16) return fail(MLORA_ERR_UNSUPPORTED, "rope_append: rotary_dim must be a multiple of 16 up to head_dim");
+  if (app && T > own_capacity) return fail(MLORA_ERR_CAPACITY, "rope_append: n_nodes exceeds own_capacity");
+  const int64_t piece = in_fp32 ? 4 : 8;                   // elements in 16 bytes
+  if ((q && (q_stride < (int64_t)Hq * hd || q_stride % piece)) || (app && (k_stride < (int64_t)Hkv * hd || k_stride % piece || v_stride < (int64_t)Hkv * hd || v_stride % piece)))
+    return fail(MLORA_ERR_ARG, "rope_append: row strides must cover a row and be multiples of 16 bytes");
+  if (misaligned16({q, k, v, q_out, own_k, own_v})) return fail(MLORA_ERR_ARG, "rope_append: tensors must be 16-byte aligned");
+  if (q && q == q_out && (in_fp32 || q_stride != (int64_t)Hq * hd)) return fail(MLORA_ERR_ARG, "rope_append: in place only for packed fp16 rows");
+  RopeArgs a{};
+  a.q = q; a.k = k; a.v = v; a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+  a.positions = positions; a.freq = freq; a.gain = gain; a.in_fp32 = in_fp32 != 0; a.interleaved = interleaved != 0; a.rotary = rotary_dim;
+  a.n = n; a.T = T; a.Hq = q ? Hq : 0; a.Hkv = app ? Hkv : 0; a.hd = hd; a.cap = own_capacity;
+  a.q_out = (__half*)q_out; a.own_k = (__half*)own_k; a.own_v = (__half*)own_v; a.suffix_len = suffix_len;
+  a.own_weight = own_weight; a.own_position = own_position; a.status = status;
+  CK(launch_rope_append(a, (cudaStream_t)cuda_stream));
+  return MLORA_OK;
+}
+
+static ScoredArgs scored_fill(int n, int T, int Hq, int Hkv, int hd, int P, int suffix_bound) {
+  ScoredArgs a{};
+  a.n = n; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.hd = hd; a.P = P; a.suffix_bound = suffix_bound;
+  scored_plan(a, 148);
+  return a;
+}
+
+static bool scored_shape(int32_t n, int32_t T, int32_t Hq, int32_t Hkv, int32_t P, int32_t suffix_bound) {
+  return n > 0 && T > 0 && T <= 64 && Hq > 0 && Hkv > 0 && Hkv <= 65535 && Hq % Hkv == 0 && P >= 0 && suffix_bound >= 0 &&
+         P < (1 << 30) && suffix_bound < (1 << 30) && (long long)n * T * Hq < (1ll << 30);
+}
+
+size_t mlora_attention_scored_workspace_bytes(int32_t n, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, int32_t P,
+                                              int32_t suffix_bound) {
+  if (!scored_shape(n, T, Hq, Hkv, P, suffix_bound) || (hd != 64 && hd != 128)) return 0;
+  // Enough for every bound up to this one too.  Chunks grow with the bound, in a few steps: within a step the need grows with
+  // the bound, so the last bound of each step decides.
+  size_t floats = 0;
+  for (int lo = 0; lo <= suffix_bound;) {
+    const int chunk = scored_fill(n, T, Hq, Hkv, hd, P, lo).own_chunk;
+    int a = lo, b = suffix_bound;                          // the last bound with this chunk
+    while (a < b) {
+      const int mid = a + (b - a + 1) / 2;
+      if (scored_fill(n, T, Hq, Hkv, hd, P, mid).own_chunk == chunk) a = mid; else b = mid - 1;
+    }
+    const size_t f = scored_workspace_floats(scored_fill(n, T, Hq, Hkv, hd, P, a));
+    floats = f > floats ? f : floats;
+    lo = a + 1;
+  }
+  return floats * sizeof(float) + 16;
+}
+
+int mlora_attention_scored(const void* q, const void* prefix_k, const void* prefix_v, int32_t P, const void* own_k,
+                           const void* own_v, int32_t own_capacity, const int32_t* suffix_len, int32_t suffix_bound,
+                           const int32_t* tree_parent, int32_t n, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, void* out,
+                           float* own_weight, float* prefix_weight, void* workspace, size_t workspace_bytes, int32_t* status,
+                           void* cuda_stream) {
+  if (!q || !own_k || !own_v || !suffix_len || !out || !own_weight || !workspace || !status) return fail(MLORA_ERR_ARG, "attention_scored: null argument");
+  if (P > 0 && (!prefix_k || !prefix_v)) return fail(MLORA_ERR_ARG, "attention_scored: null prefix");
+  if (!scored_shape(n, T, Hq, Hkv, P, suffix_bound)) return fail(MLORA_ERR_ARG, "attention_scored: bad shape");
+  if (hd != 64 && hd != 128) return fail(MLORA_ERR_UNSUPPORTED, "attention_scored: head_dim must be 64 or 128");
+  if ((long long)suffix_bound + T > own_capacity) return fail(MLORA_ERR_CAPACITY, "attention_scored: suffix_bound + n_nodes exceeds own_capacity");
+  if (misaligned16({q, prefix_k, prefix_v, own_k, own_v, out})) return fail(MLORA_ERR_ARG, "attention_scored: q, K, V and out must be 16-byte aligned");
+  ScoredArgs a = scored_fill(n, T, Hq, Hkv, hd, P, suffix_bound);
+  float* const ws = (float*)(((uintptr_t)workspace + 15) & ~(uintptr_t)15);
+  if (workspace_bytes < (size_t)((unsigned char*)ws - (unsigned char*)workspace) + scored_workspace_floats(a) * sizeof(float))
+    return fail(MLORA_ERR_CAPACITY, "attention_scored: workspace too small");
+  scored_carve(a, ws);
+  a.q = (const __half*)q; a.prefix_k = (const __half*)prefix_k; a.prefix_v = (const __half*)prefix_v;
+  a.own_k = (const __half*)own_k; a.own_v = (const __half*)own_v; a.cap = own_capacity;
+  a.suffix_len = suffix_len; a.parent = tree_parent; a.out = (__half*)out;
+  a.own_weight = own_weight; a.prefix_weight = P > 0 ? prefix_weight : nullptr; a.status = status;
+  CK(launch_attention_scored(a, (cudaStream_t)cuda_stream));
+  return MLORA_OK;
+}
+
+static int32_t evict_max_moves(int32_t suffix_bound, int32_t budget) {
+  const int32_t over = suffix_bound > budget ? suffix_bound - budget : 0;
+  return over < budget ? over : budget;
+}
+
+size_t mlora_kv_evict_workspace_bytes(int32_t n, int32_t Hkv, int32_t suffix_bound, int32_t budget) {
+  if (n <= 0 || Hkv <= 0 || suffix_bound < 0 || budget <= 0) return 0;
+  // (min(budget, bound - budget) rows move at most: never more for a smaller bound)
+  return 16 + (size_t)n * Hkv * (sizeof(int32_t) + (size_t)evict_max_moves(suffix_bound, budget) * sizeof(int2)) + 16;
+}
+
+int mlora_kv_evict(void* own_k, void* own_v, const float* own_weight, const int32_t* own_position, int32_t own_capacity,
+                   const int32_t* suffix_len, int32_t suffix_bound, const int32_t* newest, int32_t budget, int32_t recent,
+                   int32_t n, int32_t Hkv, int32_t hd, float* out_weight, int32_t* out_position, int32_t* out_len,
+                   int32_t* out_source, void* workspace, size_t workspace_bytes, int32_t* status, void* cuda_stream) {
+  if (!own_k || !own_v || !own_weight || !suffix_len || !out_weight || !out_len || !workspace || !status) return fail(MLORA_ERR_ARG, "kv_evict: null argument");
+  if ((own_position == nullptr) != (out_position == nullptr)) return fail(MLORA_ERR_ARG, "kv_evict: own_position and out_position go together");
+  if (n <= 0 || Hkv <= 0 || (long long)n * Hkv > 65535 || suffix_bound < 0 || budget <= 0) return fail(MLORA_ERR_ARG, "kv_evict: bad shape");
+  if (recent < 0 || recent > budget || (recent > 0 && (!own_position || !newest))) return fail(MLORA_ERR_ARG, "kv_evict: recent needs positions, newest and at most budget rows");
+  if (hd != 64 && hd != 128) return fail(MLORA_ERR_UNSUPPORTED, "kv_evict: head_dim must be 64 or 128");
+  if (suffix_bound > own_capacity) return fail(MLORA_ERR_CAPACITY, "kv_evict: suffix_bound exceeds own_capacity");
+  if (misaligned16({own_k, own_v})) return fail(MLORA_ERR_ARG, "kv_evict: K and V must be 16-byte aligned");
+  if (suffix_len == out_len) return fail(MLORA_ERR_ARG, "kv_evict: out_len must not be suffix_len");
+  EvictArgs a{};
+  a.own_k = (__half*)own_k; a.own_v = (__half*)own_v; a.weight = own_weight; a.position = own_position;
+  a.out_weight = out_weight; a.out_position = out_position; a.suffix_len = suffix_len; a.newest = newest; a.out_len = out_len;
+  a.out_source = out_source; a.n = n; a.Hkv = Hkv; a.hd = hd; a.cap = own_capacity; a.bound = suffix_bound; a.budget = budget;
+  a.recent = recent; a.max_moves = evict_max_moves(suffix_bound, budget); a.status = status;
+  unsigned char* const ws = (unsigned char*)(((uintptr_t)workspace + 15) & ~(uintptr_t)15);
+  const size_t counts = ((size_t)n * Hkv * sizeof(int32_t) + 15) / 16 * 16;
+  if (workspace_bytes < (size_t)(ws - (unsigned char*)workspace) + counts + (size_t)n * Hkv * a.max_moves * sizeof(int2))
+    return fail(MLORA_ERR_CAPACITY, "kv_evict: workspace too small");
+  a.counts = (int32_t*)ws; a.moves = (int2*)(ws + counts);
+  CK(launch_kv_evict(a, (cudaStream_t)cuda_stream));
   return MLORA_OK;
 }
 
