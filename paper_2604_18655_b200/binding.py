@@ -383,71 +383,32 @@ def mlora_rope_frequencies(rotary_dim, theta=1e4, scaling="plain", factor=1.0, l
     return freq, gain.value
 
 
-def _bad(what):
-    raise MloraError(-1, what)
+_native = None
 
 
-def _arg(t, dtype, shape, device, what):
-    """The address of a packed CUDA tensor of this type and shape on this device (None: no tensor); anything else is refused."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
-        _bad(f"{what}: expected a packed {dtype} tensor of shape {tuple(shape)} on CUDA device {device}, got {t.dtype} "
-             f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
-    return t.data_ptr()
-
-
-def _rows(t, rows, width, dtype, device, what):
-    """Address and row stride of rows of `width` packed features: [rows][width] or [rows][heads][head_dim]."""
-    sh, st = t.shape, t.stride()
-    if len(sh) == 3:
-        packed = st[2] == 1 and (st[1] == sh[2] or sh[1] == 1) and sh[1] * sh[2] == width
-    else:
-        packed = len(sh) == 2 and st[1] == 1 and sh[1] == width
-    if not packed or sh[0] != rows or t.dtype is not dtype or t.get_device() != device:
-        _bad(f"{what}: expected {rows} rows of {width} packed {dtype} features on CUDA device {device}, got {t.dtype} "
-             f"{tuple(sh)} with strides {st} on {t.device}")
-    return t.data_ptr(), (st[0] if rows > 1 else width)
+def _marshal():
+    """The module that checks and hands on the tensors of the calls below (once loaded: `_native`)."""
+    global _native
+    if _native is None:
+        L = lib()
+        try:
+            from . import _marshal as m
+        except ImportError as e:
+            raise RuntimeError("_marshal.so is missing or does not load: run `python -m paper_2604_18655_b200.build` first") from e
+        m.attach(*(C.cast(f, C.c_void_p).value for f in (L.mlora_rope_append, L.mlora_attention_scored, L.mlora_kv_evict, L.mlora_last_error)))
+        _native = m
+    return _native
 
 
 def mlora_rope_append(q, k, v, positions, freq, q_out, own_k, own_v, suffix_len, status, *, gain=1.0, interleaved=False,
                       own_weight=None, own_position=None):
     """q, k, v: fp16 or fp32 rows [rows][heads * head_dim] or [rows][heads][head_dim], any row stride; positions int32 [rows]; freq
     float64 [rotary_dim / 2]; q_out fp16 [rows][Hq][hd]; own_k, own_v fp16 [n][Hkv][capacity][hd]; suffix_len int32 [n].  q and q_out,
-    or k, v, own_k and own_v, may be None."""
-    dev = _get_device()
-    rows = positions.numel()
-    n, Hq, Hkv, cap = rows, 0, 0, 0
-    dtype = (k if q is None else q).dtype
-    if dtype is not torch.float32 and dtype is not torch.float16:
-        _bad(f"rope_append: rows of {dtype}")
-    if own_k is not None:
-        if k is None or v is None or own_v is None or own_k.dim() != 4:
-            _bad("rope_append: k, v, own_k [n][Hkv][capacity][hd] and own_v go together")
-        n, Hkv, cap, hd = own_k.shape
-    if q_out is not None:
-        if q is None or q_out.dim() != 3:
-            _bad("rope_append: q and q_out [rows][Hq][hd] go together")
-        Hq, hd = q_out.shape[1:]
-    if n == 0 or rows % n or (q_out is None and own_k is None):
-        _bad("rope_append: nothing to do, or rows that are no multiple of the streams")
-    qp = kp = vp = None
-    qs = ks = vs = 0
-    if q is not None:
-        qp, qs = _rows(q, rows, Hq * hd, dtype, dev, "q")
-    if k is not None:
-        kp, ks = _rows(k, rows, Hkv * hd, dtype, dev, "k")
-        vp, vs = _rows(v, rows, Hkv * hd, dtype, dev, "v")
-    i32, per_row = torch.int32, (n, Hkv, cap)
-    code = lib().mlora_rope_append(
-        qp, kp, vp, dtype is torch.float32, qs, ks, vs, _arg(positions, i32, positions.shape, dev, "positions"),
-        _arg(freq, torch.float64, (freq.numel(),), dev, "freq"), gain, 2 * freq.numel(), interleaved, n, rows // n, Hq, Hkv, hd,
-        _arg(q_out, torch.float16, (rows, Hq, hd), dev, "q_out"), _arg(own_k, torch.float16, (n, Hkv, cap, hd), dev, "own_k"),
-        _arg(own_v, torch.float16, (n, Hkv, cap, hd), dev, "own_v"), cap, _arg(suffix_len, i32, (n,), dev, "suffix_len"),
-        _arg(own_weight, torch.float32, per_row, dev, "own_weight"), _arg(own_position, i32, per_row, dev, "own_position"),
-        _arg(status, i32, (1,), dev, "status"), _raw_stream(dev))
-    if code:
-        _check(code)
+    or k, v, own_k and own_v, may be None.  Tensors of another type, shape, packing or device than the current one are refused."""
+    r = (_native or _marshal()).rope_append(q, k, v, positions, freq, q_out, own_k, own_v, suffix_len, status, gain, interleaved,
+                                            own_weight, own_position)
+    if r is not None:
+        raise MloraError(*r)
 
 
 def mlora_attention_scored_workspace_bytes(n, T, Hq, Hkv, hd, P, suffix_bound):
@@ -456,25 +417,12 @@ def mlora_attention_scored_workspace_bytes(n, T, Hq, Hkv, hd, P, suffix_bound):
 
 def mlora_attention_scored(q, prefix_k, prefix_v, own_k, own_v, suffix_len, suffix_bound, tree_parent, out, own_weight,
                            prefix_weight, workspace, status):
-    """As mlora_attention (tree_parent None: one row a stream, or a chain of q.shape[0] / n rows); own_weight fp32 [n][Hkv][capacity]
-    and prefix_weight fp32 [Hkv][P] (or None) grow by the weights that the pass gives."""
-    dev = _get_device()
-    if q.dim() != 3 or own_k.dim() != 4 or (prefix_k is not None and prefix_k.dim() != 3):
-        _bad("attention_scored: expected q [rows][Hq][hd], own_k [n][Hkv][capacity][hd], prefix_k [Hkv][P][hd]")
-    rows, Hq, hd = q.shape
-    n, Hkv, cap = own_k.shape[:3]
-    P = 0 if prefix_k is None else prefix_k.shape[1]
-    T = rows // n if n else 0
-    f16, f32, i32 = torch.float16, torch.float32, torch.int32
-    own, pre = (n, Hkv, cap, hd), (Hkv, P, hd)
-    code = lib().mlora_attention_scored(
-        _arg(q, f16, (n * T, Hq, hd), dev, "q"), _arg(prefix_k, f16, pre, dev, "prefix_k"), _arg(prefix_v, f16, pre, dev, "prefix_v"), P,
-        _arg(own_k, f16, own, dev, "own_k"), _arg(own_v, f16, own, dev, "own_v"), cap, _arg(suffix_len, i32, (n,), dev, "suffix_len"),
-        suffix_bound, _arg(tree_parent, i32, (n, T), dev, "tree_parent"), n, T, Hq, Hkv, hd, _arg(out, f16, (n * T, Hq, hd), dev, "out"),
-        _arg(own_weight, f32, (n, Hkv, cap), dev, "own_weight"), _arg(prefix_weight, f32, (Hkv, P), dev, "prefix_weight"),
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _arg(status, i32, (1,), dev, "status"), _raw_stream(dev))
-    if code:
-        _check(code)
+    """As mlora_attention (tree_parent int32 [n][T], or None: one row a stream, or a chain of q.shape[0] / n rows); own_weight fp32
+    [n][Hkv][capacity] and prefix_weight fp32 [Hkv][P] (or None) grow by the weights that the pass gives."""
+    r = (_native or _marshal()).attention_scored(q, prefix_k, prefix_v, own_k, own_v, suffix_len, suffix_bound, tree_parent, out,
+                                                 own_weight, prefix_weight, workspace, status)
+    if r is not None:
+        raise MloraError(*r)
 
 
 def mlora_kv_evict_workspace_bytes(n, Hkv, suffix_bound, budget):
@@ -486,18 +434,7 @@ def mlora_kv_evict(own_k, own_v, own_weight, own_position, suffix_len, suffix_bo
     """own_k, own_v fp16 [n][Hkv][capacity][hd]; own_weight fp32, own_position int32 (or None) [n][Hkv][capacity]; out_weight and
     out_position the same (they may be the same tensors); suffix_len, newest (or None), out_len int32 [n]; out_source int32
     [n][Hkv][budget] or None."""
-    dev = _get_device()
-    if own_k.dim() != 4:
-        _bad("kv_evict: expected own_k [n][Hkv][capacity][hd]")
-    n, Hkv, cap, hd = own_k.shape
-    f16, f32, i32 = torch.float16, torch.float32, torch.int32
-    own, per_row = own_k.shape, (n, Hkv, cap)
-    code = lib().mlora_kv_evict(
-        _arg(own_k, f16, own, dev, "own_k"), _arg(own_v, f16, own, dev, "own_v"), _arg(own_weight, f32, per_row, dev, "own_weight"),
-        _arg(own_position, i32, per_row, dev, "own_position"), cap, _arg(suffix_len, i32, (n,), dev, "suffix_len"), suffix_bound,
-        _arg(newest, i32, (n,), dev, "newest"), budget, recent, n, Hkv, hd, _arg(out_weight, f32, per_row, dev, "out_weight"),
-        _arg(out_position, i32, per_row, dev, "out_position"), _arg(out_len, i32, (n,), dev, "out_len"),
-        _arg(out_source, i32, (n, Hkv, budget), dev, "out_source"), _ptr(workspace), workspace.numel() * workspace.element_size(),
-        _arg(status, i32, (1,), dev, "status"), _raw_stream(dev))
-    if code:
-        _check(code)
+    r = (_native or _marshal()).kv_evict(own_k, own_v, own_weight, own_position, suffix_len, suffix_bound, newest, budget, recent,
+                                         out_weight, out_position, out_len, workspace, status, out_source)
+    if r is not None:
+        raise MloraError(*r)

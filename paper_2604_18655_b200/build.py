@@ -1,12 +1,15 @@
-"""Builds libmlora.so (sm_100a only) next to this file with nvcc.  No JIT cache: the library stays in-tree."""
+"""Builds libmlora.so (sm_100a only) next to this file with nvcc, and with the host compiler the module that checks and hands on the
+tensors of its cache operators.  No JIT cache: both stay in-tree."""
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["w4_gemm.cu", "lora_shrink.cu", "step_misc.cu", "attention.cu", "decode_chain.cu", "decode_step.cu", "decode_lean.cu", "w4_gemm_tc.cu", "attn_tc.cu", "w4a8_gemm.cu", "rope.cu", "attn_scored.cu", "kv_evict.cu", "mlora.cu"]
 LIB = os.path.join(HERE, "libmlora.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
 
@@ -32,6 +35,16 @@ def build(force=False, verbose=False):
         if not force and _newer(obj, [src] + headers):
             continue
         cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", src, "-o", obj]
+        procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    marshal_src = os.path.join(CSRC, "marshal.cpp")
+    if force or not _newer(MARSHAL, [marshal_src, headers[-1]]):
+        import torch
+        root = os.path.dirname(torch.__file__)
+        inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
+               os.path.join(os.path.dirname(os.path.dirname(nvcc)), "include")]
+        lib = os.path.join(root, "lib")
+        cmd = ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
+               ["-isystem" + d for d in inc] + [marshal_src, "-o", MARSHAL, "-L" + lib, "-Wl,-rpath," + lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
         procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for cmd, p in procs:
         out, _ = p.communicate()

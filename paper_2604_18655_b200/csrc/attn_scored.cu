@@ -8,8 +8,12 @@
 // (scored_rows_kernel: online softmax over a chunk of keys, partial results as in any split attention) also leaves the scores
 // in scratch, and the second one (scored_finish_kernel) joins the partials and sums exp(s - m) / sum over the rows of a key.
 // The scores are 4 bytes a row and key against 4 hd bytes of K and V: little where few rows share a KV head.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
 #include "../../include/mlora.h"
 #include "cache_ops.cuh"
+#include "tc.cuh"
 
 namespace mlora {
 
@@ -310,31 +314,344 @@ __global__ void __launch_bounds__(FIN_THREADS) scored_finish_kernel(const Scored
   if (key < limit) dst[key] += sum;
 }
 
-// Chunks: a wave or so of CTAs, from one round of keys to eight
+// ----------------------------------------------------------------------------- many rows a KV head (trees, wide groups)
+// Attention as mlora_attention runs it (attn_tc_kernel and its merge), whose partial maxima and sums then give every row's
+// normaliser; a second pass over K alone makes the scores again, on the tensor cores, and sums the weights key by key.  For 96 rows a
+// KV head the scores in scratch would be 768 bytes of traffic a key, K is 256.
+// One CTA: 128 keys of a segment against all rows that see them, up to 128 at a time.  S^T = K Q^T with the keys as the rows of
+// the accumulator: a thread owns a key (its tensor-memory lane), so that sums over query rows stay in the thread and no order of
+// work can change them.  Two accumulators: the next block's product is made while this one's exponentials are.
+// What bounds it: the exponentials, 8 clocks an SM for a row of a tile (16 a clock).
+constexpr int SW_KEYS = 128, SW_ROWS = 128, SW_SLOTS = 8, SW_THREADS = 160;
+template <int HD> struct SwCfg {
+  static constexpr uint32_t TILE = SW_KEYS * HD * 2;
+  static constexpr size_t SMEM = 3 * (size_t)TILE + 1024;
+};
+
+// the row's normaliser from its chunks' maxima and sums: (maximum, 1 / sum)
+__device__ __forceinline__ float2 sw_join(const float2* ml, int ns) {
+  float M = -INFINITY, L = 0.f;
+  for (int i = 0; i < ns; ++i) M = fmaxf(M, __ldcg(ml + i).x);
+  const float Mb = M == -INFINITY ? 0.f : M;
+  for (int i = 0; i < ns; ++i) { const float2 x = __ldcg(ml + i); L += sc_ex2(x.x - Mb) * x.y; }
+  return make_float2(Mb, 1.f / L);
+}
+
+template <int HD>
+__global__ void __launch_bounds__(SW_THREADS, 2)
+scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const int prefix_tiles, const int own_tiles, const float scale_log2,
+                      const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_pk, const __grid_constant__ CUtensorMap map_ok) {
+  constexpr int HALVES = HD / 64;
+  constexpr uint32_t TILE = SwCfg<HD>::TILE, HALF = SW_KEYS * 128;
+  extern __shared__ __align__(1024) unsigned char sw_smem[];
+  __shared__ __align__(8) uint64_t k_full, q_full[2], q_empty[2], s_full[2], s_empty[2];
+  __shared__ __align__(16) float2 ml_s[2][SW_ROWS];
+  __shared__ unsigned long long anc_s[2][SW_ROWS];
+  __shared__ uint32_t tmem_s;
+  const uint32_t k_sm = (tc_smem_u32(sw_smem) + 1023u) & ~1023u, q_sm = k_sm + TILE;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const int kh = blockIdx.y, G = p.Hq / p.Hkv, R = p.T * G, R_all = p.n * R, slots = p.attn.n_prefix_chunks + p.attn.n_own_chunks;
+  const bool own = (int)blockIdx.x >= prefix_tiles;
+  int s = 0, key0, limit, v_lo = 0, v_hi = R_all, S = 0;
+  if (own) asm volatile("griddepcontrol.wait;" ::: "memory");          // (the lengths are written by this call)
+  if (!own) {
+    key0 = blockIdx.x * SW_KEYS; limit = p.P;
+  } else {
+    const int i = blockIdx.x - prefix_tiles;
+    s = i / own_tiles; key0 = (i - s * own_tiles) * SW_KEYS;
+    S = p.lens[s]; limit = S + p.T;
+    v_lo = s * R; v_hi = v_lo + R;
+    if (key0 >= limit) return;
+  }
+  const int blocks = (v_hi - v_lo + rb - 1) / rb;
+  if (tid == 0) {
+    TC_MBAR_INIT(&k_full, 1);
+    for (int i = 0; i < 2; ++i) { TC_MBAR_INIT(q_full + i, 1); TC_MBAR_INIT(q_empty + i, 1); TC_MBAR_INIT(s_full + i, 1); TC_MBAR_INIT(s_empty + i, 4); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 4) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc_smem_u32(&tmem_s)), "r"(256u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_s, 0);
+  if (warp == 4) {
+    // ---- copies and MMAs, by one thread.  Neither K nor q is written by the kernels of this call.
+    if (tc_elect()) {
+      auto load_q = [&](int b) {
+        const uint32_t bar = tc_smem_u32(q_full + (b & 1)), dst = q_sm + (b & 1) * TILE;
+        tc_expect_tx(bar, HALVES * (uint32_t)rb * 128u);
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) at_copy3(dst + h * HALF, &map_q, h * 64, kh * G, (v_lo + b * rb) / G, bar);
+      };
+      tc_expect_tx(tc_smem_u32(&k_full), TILE);
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) {
+        if (own) at_copy4(k_sm + h * HALF, &map_ok, h * 64, key0, kh, s, tc_smem_u32(&k_full));
+        else at_copy3(k_sm + h * HALF, &map_pk, h * 64, key0, kh, tc_smem_u32(&k_full));
+      }
+      load_q(0);
+      if (blocks > 1) load_q(1);
+      constexpr uint64_t DESC = ((uint64_t)1 << 46) | ((uint64_t)2 << 61) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 16);
+      auto desc = [](uint32_t a) { return DESC | (uint64_t)((a & 0x3FFFF) >> 4); };
+      int loaded = blocks > 1 ? 2 : 1;
+      bool alive = tc_wait(tc_smem_u32(&k_full), 0u, p.status);
+      for (int b = 0; b < blocks && alive; ++b) {
+        const int st = b & 1; const uint32_t ph = (uint32_t)((b >> 1) & 1);
+        alive = tc_wait(tc_smem_u32(q_full + st), ph, p.status) && tc_wait(tc_smem_u32(s_empty + st), ph ^ 1u, p.status);
+        if (!alive) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const int n_rows = min(rb, v_hi - v_lo - b * rb);
+        const uint32_t idesc = (1u << 4) | ((uint32_t)((n_rows + 15) / 16 * 2) << 17) | ((SW_KEYS >> 4) << 24);
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) {
+          const uint32_t off = (kk >> 2) * HALF + (kk & 3) * 32;
+          asm volatile(
+              "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+              "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+              ::"r"(tmem + st * 128), "l"(desc(k_sm + off)), "l"(desc(q_sm + st * TILE + off)), "r"(idesc), "r"(kk > 0 ? 1u : 0u) : "memory");
+        }
+        tc_commit(tc_smem_u32(s_full + st));
+        tc_commit(tc_smem_u32(q_empty + st));
+        if (b + 2 < blocks) {
+          alive = tc_wait(tc_smem_u32(q_empty + st), ph, p.status);
+          if (alive) { load_q(b + 2); loaded = b + 3; }
+        }
+      }
+      // no copy may be in flight when the CTA ends (passes at once unless a wait gave up somewhere)
+      if (!alive) {
+        tc_wait(tc_smem_u32(&k_full), 0u, p.status);
+        for (int b = loaded > 2 ? loaded - 2 : 0; b < loaded; ++b) tc_wait(tc_smem_u32(q_full + (b & 1)), (uint32_t)((b >> 1) & 1), p.status);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---- weights: thread = key; a block's rows' normalisers are brought by the same threads, one row each
+    if (!own) asm volatile("griddepcontrol.wait;" ::: "memory");
+    const float2* const ml_all = reinterpret_cast<const float2*>(p.part_ml) + (size_t)kh * R_all * slots;
+    auto slots_of = [&](int v) { return p.attn.n_prefix_chunks + min(p.attn.n_own_chunks, (p.lens[v / R] + p.T + p.attn.own_chunk - 1) / p.attn.own_chunk); };
+    const int key = key0 + tid, d = key - S;
+    const bool masked = own && key0 + SW_KEYS > S && p.T > 1;          // (the same for the whole CTA)
+    bool alive = true;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    float2 next = make_float2(0.f, 0.f);
+    unsigned long long next_anc = 0ull;
+    auto fetch = [&](int b) {
+      const int v = v_lo + b * rb + tid;
+      if (tid < rb && v < v_hi) { next = sw_join(ml_all + (size_t)v * slots, slots_of(v)); if (masked) next_anc = p.anc[v / G]; }
+    };
+    fetch(0);
+    for (int b = 0; b < blocks; ++b) {
+      const int st = b & 1; const uint32_t ph = (uint32_t)((b >> 1) & 1);
+      ml_s[st][tid] = next;
+      if (masked) anc_s[st][tid] = next_anc;
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      if (b + 1 < blocks) fetch(b + 1);
+      if (alive) alive = tc_wait(tc_smem_u32(s_full + st), ph, p.status);
+      alive = __all_sync(0xffffffffu, alive);                          // (no way out: the other warps wait at the barrier)
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const int n_rows = alive ? min(rb, v_hi - v_lo - b * rb) : 0;
+      const uint32_t at = tmem + st * 128 + ((uint32_t)(warp * 32) << 16);
+      for (int c0 = 0; c0 < n_rows; c0 += 32) {
+        float x[32];
+        at_ld32(at + c0, x);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        if (c0 + 32 <= n_rows && !masked) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const float4 ml = *reinterpret_cast<const float4*>(&ml_s[st][c0 + i]);
+            sum[i & 3] = fmaf(sc_ex2(fmaf(x[i], scale_log2, -ml.x)), ml.y, sum[i & 3]);
+            sum[(i + 1) & 3] = fmaf(sc_ex2(fmaf(x[i + 1], scale_log2, -ml.z)), ml.w, sum[(i + 1) & 3]);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            if (c0 + i < n_rows) {
+              const float2 ml = ml_s[st][c0 + i];
+              const bool see = !masked || d < 0 || (d < 64 && ((anc_s[st][c0 + i] >> d) & 1ull));
+              if (see) sum[i & 3] = fmaf(sc_ex2(fmaf(x[i], scale_log2, -ml.x)), ml.y, sum[i & 3]);
+            }
+          }
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) tc_arrive(tc_smem_u32(s_empty + st));
+    }
+    if (alive && key < limit) {
+      float* dst = own ? p.own_weight + ((size_t)s * p.Hkv + kh) * p.cap : p.prefix_weight + (size_t)kh * p.P;
+      dst[key] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
+}
+
+// What the tcgen05 kernels read of the pass: lengths within their bound, every node's ancestor-or-self mask (a malformed parent
+// counts as the root, and is reported).
+__global__ void scored_prep_kernel(const ScoredArgs p) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < p.n) {
+    const int S = p.suffix_len[i];
+    if (S < 0 || S > p.suffix_bound) atomicCAS(p.status, 0, MLORA_ERR_ARG);
+    p.lens[i] = S < 0 ? 0 : (S > p.suffix_bound ? p.suffix_bound : S);
+  }
+  if (i >= p.n * p.T) return;
+  const int s = i / p.T;
+  int c = i - s * p.T;
+  unsigned long long mask = 1ull;
+  if (p.parent == nullptr) mask = c >= 63 ? ~0ull : (1ull << (c + 1)) - 1;
+  else {
+    const int32_t* par = p.parent + (size_t)s * p.T;
+    bool bad = par[0] != -1;
+    for (int it = 0; it < 64 && c > 0; ++it) {
+      mask |= 1ull << c;
+      int pc = par[c];
+      if (pc < 0 || pc >= c) { bad = true; pc = 0; }
+      c = pc;
+    }
+    if (bad) atomicCAS(p.status, 0, MLORA_ERR_ARG);
+  }
+  p.anc[i] = mask;
+}
+
+template <int HD>
+static cudaError_t sw_launch(const ScoredArgs& a, cudaStream_t st) {
+  const int rows = a.n * a.T, G = a.Hq / a.Hkv, rb = G * (SW_ROWS / G);
+  scored_prep_kernel<<<(rows + 127) / 128, 128, 0, st>>>(a);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  AttnArgs t = a.attn;
+  t.q = a.q; t.prefix_k = a.prefix_k; t.prefix_v = a.prefix_v; t.prefix_head_stride = (size_t)a.P * HD;
+  t.own_k = a.own_k; t.own_v = a.own_v; t.own_head_stride = (size_t)a.cap * HD; t.own_stream_stride = t.own_head_stride * a.Hkv;
+  t.suffix_len = a.lens; t.anc = a.anc; t.depth = a.depth; t.out = a.out; t.status = a.status; t.part_o = a.part_o; t.part_ml = a.part_ml;
+  if ((e = launch_attention(t, st)) != cudaSuccess) return e;
+  t.pdl = 1;
+  if ((e = launch_attention_merge(t, st)) != cudaSuccess) return e;
+  const cuuint64_t H = sizeof(__half);
+  CUtensorMap mq, mpk, mok;
+  {
+    const cuuint64_t d[3] = {HD, (cuuint64_t)a.Hq, (cuuint64_t)rows}, s[2] = {HD * H, a.Hq * HD * H};
+    const cuuint32_t b[3] = {64, (cuuint32_t)G, (cuuint32_t)(rb / G)};
+    if ((e = at_map(a.q, 3, d, s, b, &mq)) != cudaSuccess) return e;
+  }
+  mpk = mq;
+  if (a.P > 0) {
+    const cuuint64_t d[3] = {HD, (cuuint64_t)a.P, (cuuint64_t)a.Hkv}, s[2] = {HD * H, t.prefix_head_stride * H};
+    const cuuint32_t b[3] = {64, SW_KEYS, 1};
+    if ((e = at_map(a.prefix_k, 3, d, s, b, &mpk)) != cudaSuccess) return e;
+  }
+  {
+    const cuuint64_t d[4] = {HD, (cuuint64_t)a.cap, (cuuint64_t)a.Hkv, (cuuint64_t)a.n}, s[3] = {HD * H, t.own_head_stride * H, t.own_stream_stride * H};
+    const cuuint32_t b[4] = {64, SW_KEYS, 1, 1};
+    if ((e = at_map(a.own_k, 4, d, s, b, &mok)) != cudaSuccess) return e;
+  }
+  const int prefix_tiles = a.prefix_weight != nullptr ? (a.P + SW_KEYS - 1) / SW_KEYS : 0, own_tiles = (a.suffix_bound + a.T + SW_KEYS - 1) / SW_KEYS;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(prefix_tiles + a.n * own_tiles), (unsigned)a.Hkv);
+  cfg.blockDim = dim3(SW_THREADS); cfg.dynamicSmemBytes = SwCfg<HD>::SMEM; cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, scored_weights_kernel<HD>, a, rb, prefix_tiles, own_tiles, 1.4426950408889634f / sqrtf((float)HD), mq, mpk, mok);
+}
+
+cudaError_t init_scored() {
+  cudaError_t e;
+  if ((e = full_carveout(scored_weights_kernel<64>)) != cudaSuccess || (e = full_carveout(scored_weights_kernel<128>)) != cudaSuccess) return e;
+  if ((e = cudaFuncSetAttribute(scored_weights_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SwCfg<64>::SMEM)) != cudaSuccess) return e;
+  return cudaFuncSetAttribute(scored_weights_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SwCfg<128>::SMEM);
+}
+
+// ----------------------------------------------------------------------------- plan
+// The tcgen05 kernels from more than 16 rows a stream and KV head on.
+static bool sc_tc(const ScoredArgs& a) { const int G = a.Hq / a.Hkv; return a.T * G > 16 && G <= SW_ROWS && tensor_maps_available(); }
+
+// Few rows: chunks for a wave or so of CTAs, from one round of keys to eight
+static int sc_chunk(const ScoredArgs& a, int sm_count) {
+  const int G = a.Hq / a.Hkv, rt_own = (a.T * G + 15) / 16, rt_prefix = (a.n * a.T * G + 15) / 16;
+  const long long units = a.Hkv * (rt_prefix * (long long)a.P + (long long)a.n * rt_own * ((long long)a.suffix_bound + a.T));
+  const long long chunk = units / (sm_count * 4) / SC_KEYS * SC_KEYS;
+  return (int)(chunk < SC_KEYS ? SC_KEYS : (chunk > 8 * SC_KEYS ? 8 * SC_KEYS : chunk));
+}
+
 void scored_plan(ScoredArgs& a, int sm_count) {
   const int G = a.Hq / a.Hkv;
+  a.tc = sc_tc(a);
+  if (a.tc) {
+    a.attn = AttnArgs{};
+    a.attn.P = a.P; a.attn.n = a.n; a.attn.T = a.T; a.attn.Hq = a.Hq; a.attn.Hkv = a.Hkv; a.attn.hd = a.hd; a.attn.suffix_bound = a.suffix_bound;
+    attn_plan_tc(a.attn, sm_count);
+    return;
+  }
+  const long long own_keys = (long long)a.suffix_bound + a.T;
+  const int chunk = sc_chunk(a, sm_count);
   a.rt_own = (a.T * G + 15) / 16;
   a.rt_prefix = (a.n * a.T * G + 15) / 16;
-  const long long own_keys = (long long)a.suffix_bound + a.T;
-  const long long units = a.Hkv * (a.rt_prefix * (long long)a.P + (long long)a.n * a.rt_own * own_keys);
-  long long chunk = units / (sm_count * 4) / SC_KEYS * SC_KEYS;
-  chunk = chunk < SC_KEYS ? SC_KEYS : (chunk > 8 * SC_KEYS ? 8 * SC_KEYS : chunk);
-  a.prefix_chunk = a.own_chunk = (int)chunk;
-  a.n_prefix_chunks = (int)((a.P + chunk - 1) / chunk);
+  a.prefix_chunk = a.own_chunk = chunk;
+  a.n_prefix_chunks = (a.P + chunk - 1) / chunk;
   a.n_own_chunks = (int)((own_keys + chunk - 1) / chunk);
   a.ld_prefix = (a.P + 15) / 16 * 16;
   a.ld_own = (int)((own_keys + 15) / 16 * 16);
 }
 
-static size_t sc_parts(const ScoredArgs& a) { return (size_t)a.n * a.T * a.Hq * (a.n_prefix_chunks + a.n_own_chunks); }
-size_t scored_workspace_floats(const ScoredArgs& a) {
-  return sc_parts(a) * (a.hd + 2) + (size_t)a.n * a.T * a.Hq * ((size_t)a.ld_prefix + a.ld_own);
+static size_t sc_rows(const ScoredArgs& a) { return (size_t)a.n * a.T * a.Hq; }
+// tcgen05 form, behind the partial results: masks (two floats a node), lengths and depths
+static size_t sw_floats(const ScoredArgs& a, size_t slots) { return sc_rows(a) * slots * (a.hd + 2) + ((size_t)a.n * a.T + 1) * 4 + a.n; }
+static size_t sc_floats(const ScoredArgs& a) {
+  return sc_rows(a) * ((size_t)(a.n_prefix_chunks + a.n_own_chunks) * (a.hd + 2) + (size_t)a.ld_prefix + a.ld_own);
 }
+size_t scored_workspace_floats(const ScoredArgs& a) {
+  return a.tc ? sw_floats(a, (size_t)a.attn.n_prefix_chunks + a.attn.n_own_chunks) : sc_floats(a);
+}
+
+size_t scored_workspace_most(const ScoredArgs& given, int sm_count) {
+  ScoredArgs a = given;
+  scored_plan(a, sm_count);
+  if (a.tc) {
+    // an own segment is cut in at most so many chunks as two CTAs an SM take, or tiles
+    const int G = a.Hq / a.Hkv, rb = G * (SW_ROWS / G), per_chunk = a.Hkv * a.n * ((a.T * G + rb - 1) / rb);
+    const int tiles = (a.suffix_bound + a.T + SW_KEYS - 1) / SW_KEYS, most = 2 * sm_count / per_chunk;
+    return sw_floats(a, (size_t)a.attn.n_prefix_chunks + (tiles < most ? tiles : (most > 1 ? most : 1)));
+  }
+  // chunks grow with the bound, in a few steps, and within a step so does the need: the last bound of each step decides
+  size_t floats = 0;
+  for (int lo = 0; lo <= given.suffix_bound;) {
+    a.suffix_bound = lo;
+    const int chunk = sc_chunk(a, sm_count);
+    int x = lo, y = given.suffix_bound;
+    while (x < y) {
+      a.suffix_bound = x + (y - x + 1) / 2;
+      if (sc_chunk(a, sm_count) == chunk) x = a.suffix_bound; else y = a.suffix_bound - 1;
+    }
+    a.suffix_bound = x;
+    scored_plan(a, sm_count);
+    const size_t f = sc_floats(a);
+    floats = f > floats ? f : floats;
+    lo = x + 1;
+  }
+  return floats;
+}
+
 void scored_carve(ScoredArgs& a, float* ws) {              // ws: 16-byte aligned
   a.part_o = ws;
-  a.sc_prefix = a.part_o + sc_parts(a) * a.hd;
-  a.sc_own = a.sc_prefix + (size_t)a.n * a.T * a.Hq * a.ld_prefix;
-  a.part_ml = a.sc_own + (size_t)a.n * a.T * a.Hq * a.ld_own;
+  if (a.tc) {
+    const size_t parts = sc_rows(a) * ((size_t)a.attn.n_prefix_chunks + a.attn.n_own_chunks);
+    a.part_ml = ws + parts * a.hd;
+    float* const at = a.part_ml + (parts * 2 + 3) / 4 * 4;
+    a.anc = (unsigned long long*)at;
+    a.depth = (int32_t*)(a.anc + (size_t)a.n * a.T);
+    a.lens = a.depth + (size_t)a.n * a.T;
+    return;
+  }
+  const size_t parts = sc_rows(a) * ((size_t)a.n_prefix_chunks + a.n_own_chunks);
+  a.sc_prefix = a.part_o + parts * a.hd;
+  a.sc_own = a.sc_prefix + sc_rows(a) * a.ld_prefix;
+  a.part_ml = a.sc_own + sc_rows(a) * a.ld_own;
 }
 
 template <int HD>
@@ -350,6 +667,9 @@ static cudaError_t sc_launch(const ScoredArgs& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-cudaError_t launch_attention_scored(const ScoredArgs& a, cudaStream_t st) { return a.hd == 64 ? sc_launch<64>(a, st) : sc_launch<128>(a, st); }
+cudaError_t launch_attention_scored(const ScoredArgs& a, cudaStream_t st) {
+  if (a.tc) return a.hd == 64 ? sw_launch<64>(a, st) : sw_launch<128>(a, st);
+  return a.hd == 64 ? sc_launch<64>(a, st) : sc_launch<128>(a, st);
+}
 
 }  // namespace mlora

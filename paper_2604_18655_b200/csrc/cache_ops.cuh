@@ -34,9 +34,15 @@ struct ScoredArgs {
   int ld_prefix, ld_own;                // keys a row of the score scratch has room for
   // scratch
   float *part_o, *part_ml, *sc_prefix, *sc_own;
+  int tc;                               // many rows a KV head: the tcgen05 kernels
+  AttnArgs attn;                        // ... their attention
+  unsigned long long* anc;              // ... scratch: ancestor masks, clamped lengths, depths (not read)
+  int32_t *lens, *depth;
 };
+cudaError_t init_scored();              // per device, once
 void scored_plan(ScoredArgs& a, int sm_count);
-size_t scored_workspace_floats(const ScoredArgs& a);
+size_t scored_workspace_floats(const ScoredArgs& a);       // of a planned call
+size_t scored_workspace_most(const ScoredArgs& a, int sm_count);   // of any call with this suffix_bound or a smaller one
 void scored_carve(ScoredArgs& a, float* ws);
 cudaError_t launch_attention_scored(const ScoredArgs& a, cudaStream_t st);
 

@@ -728,6 +728,7 @@ int init_kernels() {
   CK(init_step());
   CK(init_gemm_tc());
   CK(init_attention_tc());
+  CK(init_scored());
   done = true;
   return MLORA_OK;
 }
@@ -2061,20 +2062,9 @@ static bool scored_shape(int32_t n, int32_t T, int32_t Hq, int32_t Hkv, int32_t 
 size_t mlora_attention_scored_workspace_bytes(int32_t n, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, int32_t P,
                                               int32_t suffix_bound) {
   if (!scored_shape(n, T, Hq, Hkv, P, suffix_bound) || (hd != 64 && hd != 128)) return 0;
-  // Enough for every bound up to this one too.  Chunks grow with the bound, in a few steps: within a step the need grows with
-  // the bound, so the last bound of each step decides.
-  size_t floats = 0;
-  for (int lo = 0; lo <= suffix_bound;) {
-    const int chunk = scored_fill(n, T, Hq, Hkv, hd, P, lo).own_chunk;
-    int a = lo, b = suffix_bound;                          // the last bound with this chunk
-    while (a < b) {
-      const int mid = a + (b - a + 1) / 2;
-      if (scored_fill(n, T, Hq, Hkv, hd, P, mid).own_chunk == chunk) a = mid; else b = mid - 1;
-    }
-    const size_t f = scored_workspace_floats(scored_fill(n, T, Hq, Hkv, hd, P, a));
-    floats = f > floats ? f : floats;
-    lo = a + 1;
-  }
+  ScoredArgs a{};
+  a.n = n; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.hd = hd; a.P = P; a.suffix_bound = suffix_bound;
+  const size_t floats = scored_workspace_most(a, 148);
   return floats * sizeof(float) + 16;
 }
 
@@ -2093,6 +2083,7 @@ int mlora_attention_scored(const void* q, const void* prefix_k, const void* pref
   float* const ws = (float*)(((uintptr_t)workspace + 15) & ~(uintptr_t)15);
   if (workspace_bytes < (size_t)((unsigned char*)ws - (unsigned char*)workspace) + scored_workspace_floats(a) * sizeof(float))
     return fail(MLORA_ERR_CAPACITY, "attention_scored: workspace too small");
+  if (init_kernels() != MLORA_OK) return MLORA_ERR_CUDA;
   scored_carve(a, ws);
   a.q = (const __half*)q; a.prefix_k = (const __half*)prefix_k; a.prefix_v = (const __half*)prefix_v;
   a.own_k = (const __half*)own_k; a.own_v = (const __half*)own_v; a.cap = own_capacity;

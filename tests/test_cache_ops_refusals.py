@@ -163,3 +163,27 @@ def test_evict_workspace_grows_with_the_bound(mb):
     assert sizes == sorted(sizes) and sizes[0] > 0
     assert need(4, 8, 256, 256) < need(4, 8, 257, 256) and need(4, 8, 512, 256) == need(4, 8, 100000, 256)
     assert need(0, 8, 5, 5) == 0 and need(4, 8, 5, 0) == 0
+
+
+# ------------------------------------------------------------------ the binding's own checks that need no GPU
+def test_binding_refuses_host_tensors_and_other_objects(mb):
+    import torch
+    z = lambda *s, t=torch.float16: torch.zeros(*s, dtype=t)  # noqa: E731
+    i = lambda *s: z(*s, t=torch.int32)  # noqa: E731
+    own, row = z(1, 2, 8, 64), z(1, 2, 64)
+    calls = [
+        lambda: mb.mlora_rope_append(row, row, row, i(1), z(32, t=torch.float64), row, own, own, i(1), i(1)),
+        lambda: mb.mlora_rope_append(None, None, None, i(1), z(32, t=torch.float64), None, None, None, None, None),
+        lambda: mb.mlora_rope_append(row, None, row, i(1), z(32, t=torch.float64), row, own, own, i(1), i(1)),
+        lambda: mb.mlora_rope_append(row, row, row, 5, z(32, t=torch.float64), row, own, own, i(1), i(1)),
+        lambda: mb.mlora_attention_scored(row, None, None, own, own, i(1), 7, None, row, z(1, 2, 8), None, i(9), i(1)),
+        lambda: mb.mlora_attention_scored([1], None, None, own, own, i(1), 7, None, row, z(1, 2, 8), None, i(9), i(1)),
+        lambda: mb.mlora_attention_scored(row, None, None, row, own, i(1), 7, None, row, z(1, 2, 8), None, i(9), i(1)),
+        lambda: mb.mlora_kv_evict(own, own, z(1, 2, 8), i(1, 2, 8), i(1), 8, i(1), 4, 0, z(1, 2, 8), i(1, 2, 8), i(1), i(99), i(1)),
+        lambda: mb.mlora_kv_evict(row, own, z(1, 2, 8), i(1, 2, 8), i(1), 8, i(1), 4, 0, z(1, 2, 8), i(1, 2, 8), i(1), i(99), i(1)),
+        lambda: mb.mlora_kv_evict(None, own, None, None, None, 8, None, 4, 0, None, None, None, None, None),
+    ]
+    for call in calls:
+        with pytest.raises(mb.MloraError) as e:
+            call()
+        assert e.value.code == ARG and len(str(e.value)) > 20
