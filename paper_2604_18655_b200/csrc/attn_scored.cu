@@ -26,17 +26,28 @@ __device__ __forceinline__ float sc_ex2(float x) {
   return y;
 }
 
-// One CTA: 16 query rows of a kv head against a chunk of keys, the warps taking 16 keys in turn.
-// K and V go straight from global memory to the fragments of mma.m16n8k16.  A product does not depend on the order of its
-// features, nor an output on the order of its columns, so both are dealt such that a lane reads 16 bytes at a time:
-//   S:  lane (g, t) holds, of key g, the pieces 4 j + t of 8 features; a piece feeds two k-steps (q is dealt the same way)
+// One CTA: 16 query rows of a kv head against a chunk of keys, the warps taking 16 keys in turn, each through a ring of its own
+// in shared memory that it fills with 16-byte asynchronous copies (keys past the end as zeros): STAGES - 1 steps ahead, and no warp
+// waits for another before the end.  The pieces of a row lie as with the 128-byte swizzle: piece i of key k at i ^ (k mod 8).
+// From there to the fragments of mma.m16n8k16 with 16-byte reads, free of bank conflicts.  A product does not depend on the
+// order of its features, nor an output on the order of its columns, so both are dealt to suit them:
+//   S:  lane (g, t) holds, of key g, the pieces 2 t + j of each 64 features; a piece feeds two k-steps (q is dealt the same way)
 //   PV: lane (g, t) holds, of keys 2t, 2t + 1, 2t + 8, 2t + 9, piece g of each 64 features; column g of n-tile i is feature 8 g + i
+// Bound by the bytes of K and V: 8 hd16 rows ...
+template <int HD> struct ScCfg {
+  static constexpr int STAGES = HD == 64 ? 4 : 3, CTAS = HD == 64 ? 3 : 2;       // ring of a warp; CTAs an SM
+  static constexpr int STEP = 2 * SC_STEP * HD * 2;                              // bytes of a step: 16 keys' K and V
+  static constexpr size_t SMEM = (size_t)SC_WARPS * STAGES * STEP;
+};
+
 template <int HD>
-__global__ void __launch_bounds__(SC_WARPS * 32) scored_rows_kernel(const ScoredArgs p, const float scale_log2) {
-  constexpr int KP = HD / 32, HALVES = HD / 64;            // K pieces of a lane and key, 64-feature halves of V
-  __shared__ float o_s[SC_WARPS][16][HD];
+__global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_kernel(const ScoredArgs p, const float scale_log2) {
+  using C = ScCfg<HD>;
+  constexpr int HALVES = HD / 64, KP = 2 * HALVES;         // 64-feature halves; K pieces of a lane and key
+  extern __shared__ __align__(128) unsigned char sc_smem[];
   __shared__ float2 ml_s[SC_WARPS][16];
   __shared__ unsigned long long anc_s[16];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // (scored_finish_kernel, which waits for this one)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int kh = blockIdx.y, G = p.Hq / p.Hkv, R_all = p.n * p.T * G, slots = p.n_prefix_chunks + p.n_own_chunks;
   // ---- which rows, which keys
@@ -88,6 +99,28 @@ __global__ void __launch_bounds__(SC_WARPS * 32) scored_rows_kernel(const Scored
     }
     if (p.T > 1 && k1 > S) __syncthreads();
   }
+  // ---- the ring: a lane copies one piece of every RPI-th row
+  const uint32_t ring = tc_smem_u32(sc_smem) + warp * C::STAGES * C::STEP;
+  constexpr int LPR = HD / 8, RPI = 32 / LPR;              // lanes a row, rows an instruction
+  const int c_row = lane / LPR, c_piece = lane % LPR;
+  const int steps = (k1 - k0 - warp * SC_STEP + SC_KEYS - 1) / SC_KEYS;           // (may be negative: none)
+  auto copy = [&](int i) {                                 // step i of this warp
+    if (i < steps) {
+      const int key0 = k0 + (i * SC_WARPS + warp) * SC_STEP;
+      const uint32_t dst = ring + (i % C::STAGES) * C::STEP;
+#pragma unroll
+      for (int r = 0; r < SC_STEP; r += RPI) {
+        const int row = r + c_row, key = key0 + row, n = key < k1 ? 16 : 0;
+        const uint32_t at = dst + (c_piece >> 3) * (SC_STEP * 128) + row * 128 + (((c_piece & 7) ^ (row & 7)) << 4);
+        const size_t from = (size_t)(key < k1 ? key : k0) * HD + c_piece * 8;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(kb + from), "r"(n) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + SC_STEP * HD * 2), "l"(vb + from), "r"(n) : "memory");
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");   // (one a step, empty ones too: the count stays)
+  };
+#pragma unroll
+  for (int i = 0; i < C::STAGES - 1; ++i) copy(i);
   // ---- q, rows g and g + 8
   const int va = v0 + g, vz = v0 + g + 8;
   const bool ok_a = va < v1, ok_z = vz < v1;
@@ -95,57 +128,45 @@ __global__ void __launch_bounds__(SC_WARPS * 32) scored_rows_kernel(const Scored
   auto q_row = [&](int v) { const int m = v / G; return p.q + ((size_t)m * p.Hq + kh * G + (v - m * G)) * HD; };
 #pragma unroll
   for (int j = 0; j < KP; ++j) {
+    const int f = (j >> 1) * 64 + (2 * t + (j & 1)) * 8;
     uint4 a = make_uint4(0, 0, 0, 0), z = a;
-    if (ok_a) a = *reinterpret_cast<const uint4*>(q_row(va) + j * 32 + t * 8);
-    if (ok_z) z = *reinterpret_cast<const uint4*>(q_row(vz) + j * 32 + t * 8);
+    if (ok_a) a = *reinterpret_cast<const uint4*>(q_row(va) + f);
+    if (ok_z) z = *reinterpret_cast<const uint4*>(q_row(vz) + f);
     qf[2 * j][0] = a.x; qf[2 * j][1] = z.x; qf[2 * j][2] = a.y; qf[2 * j][3] = z.y;
     qf[2 * j + 1][0] = a.z; qf[2 * j + 1][1] = z.z; qf[2 * j + 1][2] = a.w; qf[2 * j + 1][3] = z.w;
   }
   unsigned long long anc_a = ~0ull, anc_z = ~0ull;
   const bool tree = own && p.T > 1 && k1 > S;
   if (tree) { anc_a = anc_s[g]; anc_z = anc_s[g + 8]; }
-  // ---- keys
-  uint4 kf[2][KP], vf[4][HALVES];
-  const uint4 zero = make_uint4(0, 0, 0, 0);
-  auto load_k = [&](int key0) {
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-      const int key = key0 + nt * 8 + g;
-#pragma unroll
-      for (int j = 0; j < KP; ++j)
-        kf[nt][j] = key < k1 ? __ldcs(reinterpret_cast<const uint4*>(kb + (size_t)key * HD + j * 32 + t * 8)) : zero;
-    }
-  };
-  auto load_v = [&](int key0) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = key0 + 2 * t + (i & 1) + (i >> 1) * 8;
-#pragma unroll
-      for (int h = 0; h < HALVES; ++h)
-        vf[i][h] = key < k1 ? __ldcs(reinterpret_cast<const uint4*>(vb + (size_t)key * HD + h * 64 + g * 8)) : zero;
-    }
-  };
   float o[HALVES * 8][4];
 #pragma unroll
   for (int i = 0; i < HALVES * 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
   float m_a = -INFINITY, m_z = -INFINITY, l_a = 0.f, l_z = 0.f;
   float* const sc_a = sc + ((size_t)kh * R_all + va) * ld;
   float* const sc_z = sc + ((size_t)kh * R_all + vz) * ld;
-  int key0 = k0 + warp * SC_STEP;
-  if (key0 < k1) { load_k(key0); load_v(key0); }
-  for (; key0 < k1; key0 += SC_KEYS) {
+  auto piece = [&](uint32_t tile, int row, int h, int i) {
+    uint4 x;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+                 : "r"(tile + h * (SC_STEP * 128) + row * 128 + ((i ^ (row & 7)) << 4)) : "memory");
+    return x;
+  };
+  for (int i = 0; i < steps; ++i) {
+    const int key0 = k0 + (i * SC_WARPS + warp) * SC_STEP;
+    asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 2) : "memory");
+    __syncwarp();                                          // (step i is there for all lanes; step i - 1's stage is free)
+    copy(i + C::STAGES - 1);
+    const uint32_t kt = ring + (i % C::STAGES) * C::STEP, vt = kt + SC_STEP * HD * 2;
     float s[2][4];
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {
       s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
       for (int j = 0; j < KP; ++j) {
-        mma_16816(s[nt], qf[2 * j], kf[nt][j].x, kf[nt][j].y);
-        mma_16816(s[nt], qf[2 * j + 1], kf[nt][j].z, kf[nt][j].w);
+        const uint4 kf = piece(kt, nt * 8 + g, j >> 1, 2 * t + (j & 1));
+        mma_16816(s[nt], qf[2 * j], kf.x, kf.y);
+        mma_16816(s[nt], qf[2 * j + 1], kf.z, kf.w);
       }
     }
-    const int next = key0 + SC_KEYS;
-    if (next < k1) load_k(next);
     float mx_a = -INFINITY, mx_z = -INFINITY;
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt)
@@ -186,16 +207,20 @@ __global__ void __launch_bounds__(SC_WARPS * 32) scored_rows_kernel(const Scored
     }
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) {
-      const uint32_t w0[4] = {vf[0][h].x, vf[0][h].y, vf[0][h].z, vf[0][h].w}, w1[4] = {vf[1][h].x, vf[1][h].y, vf[1][h].z, vf[1][h].w};
-      const uint32_t w2[4] = {vf[2][h].x, vf[2][h].y, vf[2][h].z, vf[2][h].w}, w3[4] = {vf[3][h].x, vf[3][h].y, vf[3][h].z, vf[3][h].w};
+      const uint4 x0 = piece(vt, 2 * t, h, g), x1 = piece(vt, 2 * t + 1, h, g), x2 = piece(vt, 2 * t + 8, h, g), x3 = piece(vt, 2 * t + 9, h, g);
+      const uint32_t w0[4] = {x0.x, x0.y, x0.z, x0.w}, w1[4] = {x1.x, x1.y, x1.z, x1.w};
+      const uint32_t w2[4] = {x2.x, x2.y, x2.z, x2.w}, w3[4] = {x3.x, x3.y, x3.z, x3.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        mma_16816(o[h * 8 + 2 * i], pf, __byte_perm(w0[i], w1[i], 0x5410), __byte_perm(w2[i], w3[i], 0x5410));
-        mma_16816(o[h * 8 + 2 * i + 1], pf, __byte_perm(w0[i], w1[i], 0x7632), __byte_perm(w2[i], w3[i], 0x7632));
+      for (int e = 0; e < 4; ++e) {
+        mma_16816(o[h * 8 + 2 * e], pf, __byte_perm(w0[e], w1[e], 0x5410), __byte_perm(w2[e], w3[e], 0x5410));
+        mma_16816(o[h * 8 + 2 * e + 1], pf, __byte_perm(w0[e], w1[e], 0x7632), __byte_perm(w2[e], w3[e], 0x7632));
       }
     }
-    if (next < k1) load_v(next);
   }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();                                         // the rings become the warps' outputs, [SC_WARPS][16][HD]
+  float* const o_s = reinterpret_cast<float*>(sc_smem);
+  auto o_at = [&](int w, int r, int f) -> float& { return o_s[(w * 16 + r) * HD + f]; };
   // ---- the warps' results joined
 #pragma unroll
   for (int x = 1; x <= 2; x <<= 1) {
@@ -207,8 +232,8 @@ __global__ void __launch_bounds__(SC_WARPS * 32) scored_rows_kernel(const Scored
 #pragma unroll
     for (int i = 0; i < 8; ++i) {                          // columns 2t, 2t + 1 of n-tile i: features 16 t + i, 16 t + 8 + i
       const int f = h * 64 + 16 * t + i;
-      o_s[warp][g][f] = o[h * 8 + i][0]; o_s[warp][g][f + 8] = o[h * 8 + i][1];
-      o_s[warp][g + 8][f] = o[h * 8 + i][2]; o_s[warp][g + 8][f + 8] = o[h * 8 + i][3];
+      o_at(warp, g, f) = o[h * 8 + i][0]; o_at(warp, g, f + 8) = o[h * 8 + i][1];
+      o_at(warp, g + 8, f) = o[h * 8 + i][2]; o_at(warp, g + 8, f + 8) = o[h * 8 + i][3];
     }
   if (t == 0) { ml_s[warp][g] = make_float2(m_a, l_a); ml_s[warp][g + 8] = make_float2(m_z, l_z); }
   __syncthreads();
@@ -224,7 +249,7 @@ __global__ void __launch_bounds__(SC_WARPS * 32) scored_rows_kernel(const Scored
     for (int x = 0; x < SC_WARPS; ++x) {
       const float2 ml = ml_s[x][r];
       const float f = sc_ex2(ml.x - Mb);
-      const float4 b = *reinterpret_cast<const float4*>(&o_s[x][r][c]);
+      const float4 b = *reinterpret_cast<const float4*>(&o_at(x, r, c));
       L += f * ml.y;
       a.x += f * b.x; a.y += f * b.y; a.z += f * b.z; a.w += f * b.w;
     }
@@ -234,43 +259,62 @@ __global__ void __launch_bounds__(SC_WARPS * 32) scored_rows_kernel(const Scored
   }
 }
 
-constexpr int FIN_THREADS = 128;
+constexpr int FIN_THREADS = 128, FIN_KEYS = 4 * FIN_THREADS;
 constexpr int FIN_ROWS = 256;                              // rows whose maximum and 1 / sum are held at a time
 
-// slots of row v that were written
+__device__ __forceinline__ int sc_len(const ScoredArgs& p, int s) {
+  const int S = p.suffix_len[s];
+  return S < 0 ? 0 : (S > p.suffix_bound ? p.suffix_bound : S);
+}
+// slots of a row of stream s that were written
 __device__ __forceinline__ int sc_slots(const ScoredArgs& p, int s) {
-  int S = p.suffix_len[s];
-  S = S < 0 ? 0 : (S > p.suffix_bound ? p.suffix_bound : S);
-  return p.n_prefix_chunks + min(p.n_own_chunks, (S + p.T + p.own_chunk - 1) / p.own_chunk);
+  return p.n_prefix_chunks + min(p.n_own_chunks, (sc_len(p, s) + p.T + p.own_chunk - 1) / p.own_chunk);
 }
 
-// blocks: rows of the output (one warp a row), then the prefix keys (one thread a key), then the own keys
+// Blocks: rows of the output (one warp a row), then the prefix keys (four a thread), then the own keys.  A row's chunks are joined
+// by several lanes at once: one read's latency for all of them.
 template <int HD>
 __global__ void __launch_bounds__(FIN_THREADS) scored_finish_kernel(const ScoredArgs p, const int out_blocks, const int prefix_blocks, const int own_blocks) {
   __shared__ float2 row_s[FIN_ROWS];
   const int tid = threadIdx.x, lane = tid & 31, G = p.Hq / p.Hkv, R = p.T * G, R_all = p.n * R, slots = p.n_prefix_chunks + p.n_own_chunks;
   const float2* const ml_all = reinterpret_cast<const float2*>(p.part_ml);
   int b = blockIdx.x;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   if (b < out_blocks) {
+    constexpr int F = HD / 32;                             // features of a lane
     const int w = b * (FIN_THREADS / 32) + (tid >> 5);
     if (w >= p.Hkv * R_all) return;
     const int kh = w / R_all, v = w - kh * R_all, m = v / G, ns = sc_slots(p, m / p.T);
     const size_t at = (size_t)w * slots;
-    float M = -INFINITY, L = 0.f;
-    for (int i = 0; i < ns; ++i) M = fmaxf(M, ml_all[at + i].x);
-    const float Mb = M == -INFINITY ? 0.f : M;
-    float a[HD / 32] = {};
-    for (int i = 0; i < ns; ++i) {
-      const float2 ml = ml_all[at + i];
-      const float f = sc_ex2(ml.x - Mb);
-      L += f * ml.y;
+    float M = -INFINITY, L = 0.f, a[F] = {};
+    for (int i0 = 0; i0 < ns; i0 += 32) {                  // 32 slots at a time, in order
+      const float2 ml = i0 + lane < ns ? __ldcg(ml_all + at + i0 + lane) : make_float2(-INFINITY, 0.f);
+      float x = ml.x;
 #pragma unroll
-      for (int j = 0; j < HD / 32; ++j) a[j] += f * p.part_o[(at + i) * HD + lane * (HD / 32) + j];
+      for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+      const float Mn = fmaxf(M, x), Mb = Mn == -INFINITY ? 0.f : Mn, f0 = sc_ex2(M - Mb), fl = sc_ex2(ml.x - Mb);
+      M = Mn;
+      L = L * f0 + warp_sum(fl * ml.y);
+#pragma unroll
+      for (int j = 0; j < F; ++j) a[j] *= f0;
+      const int n = min(32, ns - i0);
+      const float* po = p.part_o + (at + i0) * HD + lane * F;
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) {
+        const float f = __shfl_sync(0xffffffffu, fl, i);
+        if constexpr (F == 4) {
+          const float4 x4 = __ldcg(reinterpret_cast<const float4*>(po + (size_t)i * HD));
+          a[0] = fmaf(f, x4.x, a[0]); a[1] = fmaf(f, x4.y, a[1]); a[2] = fmaf(f, x4.z, a[2]); a[3] = fmaf(f, x4.w, a[3]);
+        } else {
+          const float2 x2 = __ldcg(reinterpret_cast<const float2*>(po + (size_t)i * HD));
+          a[0] = fmaf(f, x2.x, a[0]); a[1] = fmaf(f, x2.y, a[1]);
+        }
+      }
     }
     const float inv = 1.f / L;
-    __half2* dst = reinterpret_cast<__half2*>(p.out + ((size_t)m * p.Hq + kh * G + (v - m * G)) * HD + lane * (HD / 32));
+    __half2* dst = reinterpret_cast<__half2*>(p.out + ((size_t)m * p.Hq + kh * G + (v - m * G)) * HD + lane * F);
 #pragma unroll
-    for (int j = 0; j < HD / 64; ++j) dst[j] = __floats2half2_rn(a[2 * j] * inv, a[2 * j + 1] * inv);
+    for (int j = 0; j < F / 2; ++j) dst[j] = __floats2half2_rn(a[2 * j] * inv, a[2 * j + 1] * inv);
     return;
   }
   b -= out_blocks;
@@ -278,40 +322,56 @@ __global__ void __launch_bounds__(FIN_THREADS) scored_finish_kernel(const Scored
   const float* sc;
   float* dst;
   if (b < p.Hkv * prefix_blocks) {
-    kh = b / prefix_blocks; key = (b - kh * prefix_blocks) * FIN_THREADS + tid;
+    kh = b / prefix_blocks; key = (b - kh * prefix_blocks) * FIN_KEYS + 4 * tid;
     v0 = 0; v1 = R_all; ld = p.ld_prefix; sc = p.sc_prefix; limit = p.P;
     dst = p.prefix_weight + (size_t)kh * p.P;
   } else {
     b -= p.Hkv * prefix_blocks;
     const int seg = b / own_blocks;
-    kh = seg % p.Hkv; s = seg / p.Hkv; key = (b - seg * own_blocks) * FIN_THREADS + tid;
+    kh = seg % p.Hkv; s = seg / p.Hkv; key = (b - seg * own_blocks) * FIN_KEYS + 4 * tid;
     v0 = s * R; v1 = v0 + R; ld = p.ld_own; sc = p.sc_own;
-    int S = p.suffix_len[s];
-    limit = (S < 0 ? 0 : (S > p.suffix_bound ? p.suffix_bound : S)) + p.T;
-    if (key - tid >= limit) return;
+    limit = sc_len(p, s) + p.T;
+    if (key - 4 * tid >= limit) return;
     dst = p.own_weight + ((size_t)s * p.Hkv + kh) * p.cap;
   }
-  float sum = 0.f;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
   for (int r0 = v0; r0 < v1; r0 += FIN_ROWS) {
     const int rows = min(FIN_ROWS, v1 - r0);
     __syncthreads();
-    for (int r = tid; r < rows; r += FIN_THREADS) {
-      const int v = r0 + r, ns = sc_slots(p, v / R);
-      const size_t at = ((size_t)kh * R_all + v) * slots;
+    for (int r = tid >> 3; r < ((rows + 15) & ~15); r += FIN_THREADS / 8) {      // eight lanes a row
+      const int v = r0 + min(r, rows - 1), ns = sc_slots(p, v / R), l = lane & 7;
+      const float2* const at = ml_all + ((size_t)kh * R_all + v) * slots;
       float M = -INFINITY, L = 0.f;
-      for (int i = 0; i < ns; ++i) M = fmaxf(M, ml_all[at + i].x);
-      const float Mb = M == -INFINITY ? 0.f : M;
-      for (int i = 0; i < ns; ++i) { const float2 ml = ml_all[at + i]; L += sc_ex2(ml.x - Mb) * ml.y; }
-      row_s[r] = make_float2(Mb, 1.f / L);
+      for (int i = l; i < ns; i += 8) {
+        const float2 ml = __ldcg(at + i);
+        const float Mn = fmaxf(M, ml.x), Mb = Mn == -INFINITY ? 0.f : Mn;
+        L = L * sc_ex2(M - Mb) + ml.y * sc_ex2(ml.x - Mb);
+        M = Mn;
+      }
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) {
+        const float Mo = __shfl_xor_sync(0xffffffffu, M, o), Lo = __shfl_xor_sync(0xffffffffu, L, o);
+        const float Mn = fmaxf(M, Mo), Mb = Mn == -INFINITY ? 0.f : Mn;
+        L = L * sc_ex2(M - Mb) + Lo * sc_ex2(Mo - Mb);
+        M = Mn;
+      }
+      if (l == 0 && r < rows) row_s[r] = make_float2(M == -INFINITY ? 0.f : M, 1.f / L);
     }
     __syncthreads();
     if (key < limit) {
       const float* at = sc + ((size_t)kh * R_all + r0) * ld + key;
 #pragma unroll 4
-      for (int r = 0; r < rows; ++r) { const float2 ml = row_s[r]; sum = fmaf(sc_ex2(at[(size_t)r * ld] - ml.x), ml.y, sum); }
+      for (int r = 0; r < rows; ++r) {
+        const float2 ml = row_s[r];
+        const float4 x = __ldcg(reinterpret_cast<const float4*>(at + (size_t)r * ld));
+        sum[0] = fmaf(sc_ex2(x.x - ml.x), ml.y, sum[0]); sum[1] = fmaf(sc_ex2(x.y - ml.x), ml.y, sum[1]);
+        sum[2] = fmaf(sc_ex2(x.z - ml.x), ml.y, sum[2]); sum[3] = fmaf(sc_ex2(x.w - ml.x), ml.y, sum[3]);
+      }
     }
   }
-  if (key < limit) dst[key] += sum;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (key + i < limit) dst[key + i] += sum[i];
 }
 
 // ----------------------------------------------------------------------------- many rows a KV head (trees, wide groups)
@@ -563,6 +623,10 @@ static cudaError_t sw_launch(const ScoredArgs& a, cudaStream_t st) {
 cudaError_t init_scored() {
   cudaError_t e;
   if ((e = full_carveout(scored_weights_kernel<64>)) != cudaSuccess || (e = full_carveout(scored_weights_kernel<128>)) != cudaSuccess) return e;
+  if ((e = full_carveout(scored_rows_kernel<64>)) != cudaSuccess || (e = full_carveout(scored_rows_kernel<128>)) != cudaSuccess) return e;
+  if ((e = full_carveout(scored_finish_kernel<64>)) != cudaSuccess || (e = full_carveout(scored_finish_kernel<128>)) != cudaSuccess) return e;
+  if ((e = cudaFuncSetAttribute(scored_rows_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ScCfg<64>::SMEM)) != cudaSuccess) return e;
+  if ((e = cudaFuncSetAttribute(scored_rows_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ScCfg<128>::SMEM)) != cudaSuccess) return e;
   if ((e = cudaFuncSetAttribute(scored_weights_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SwCfg<64>::SMEM)) != cudaSuccess) return e;
   return cudaFuncSetAttribute(scored_weights_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SwCfg<128>::SMEM);
 }
@@ -571,12 +635,20 @@ cudaError_t init_scored() {
 // The tcgen05 kernels from more than 16 rows a stream and KV head on.
 static bool sc_tc(const ScoredArgs& a) { const int G = a.Hq / a.Hkv; return a.T * G > 16 && G <= SW_ROWS && tensor_maps_available(); }
 
-// Few rows: chunks for a wave or so of CTAs, from one round of keys to eight
+// Few rows: the keys in chunks that make one wave of CTAs where that is possible (chunks of at least a round of keys), else
+// four waves.  `work` = keys times 16-row tiles of all KV heads.
+static int sc_resident(const ScoredArgs& a, int sm_count) { return sm_count * (a.hd == 64 ? ScCfg<64>::CTAS : ScCfg<128>::CTAS); }
+static long long sc_work(const ScoredArgs& a) {
+  return a.Hkv * (a.rt_prefix * (long long)a.P + (long long)a.n * a.rt_own * ((long long)a.suffix_bound + a.T));
+}
 static int sc_chunk(const ScoredArgs& a, int sm_count) {
-  const int G = a.Hq / a.Hkv, rt_own = (a.T * G + 15) / 16, rt_prefix = (a.n * a.T * G + 15) / 16;
-  const long long units = a.Hkv * (rt_prefix * (long long)a.P + (long long)a.n * rt_own * ((long long)a.suffix_bound + a.T));
-  const long long chunk = units / (sm_count * 4) / SC_KEYS * SC_KEYS;
-  return (int)(chunk < SC_KEYS ? SC_KEYS : (chunk > 8 * SC_KEYS ? 8 * SC_KEYS : chunk));
+  const long long resident = sc_resident(a, sm_count), work = sc_work(a), own_keys = (long long)a.suffix_bound + a.T;
+  const long long own_items = (long long)a.Hkv * a.n * a.rt_own, prefix_items = a.P > 0 ? (long long)a.Hkv * a.rt_prefix : 0;
+  auto up = [](long long x, long long y) { return (x + y - 1) / y; };
+  if (own_items + prefix_items > resident) return (int)(up(work, 4 * resident * SC_KEYS) * SC_KEYS);
+  long long chunk = up(work, resident * SC_KEYS) * SC_KEYS;
+  while (own_items * up(own_keys, chunk) + prefix_items * up(a.P, chunk) > resident) chunk += up(chunk, 16 * SC_KEYS) * SC_KEYS;
+  return (int)chunk;
 }
 
 void scored_plan(ScoredArgs& a, int sm_count) {
@@ -589,9 +661,9 @@ void scored_plan(ScoredArgs& a, int sm_count) {
     return;
   }
   const long long own_keys = (long long)a.suffix_bound + a.T;
-  const int chunk = sc_chunk(a, sm_count);
   a.rt_own = (a.T * G + 15) / 16;
   a.rt_prefix = (a.n * a.T * G + 15) / 16;
+  const int chunk = sc_chunk(a, sm_count);
   a.prefix_chunk = a.own_chunk = chunk;
   a.n_prefix_chunks = (a.P + chunk - 1) / chunk;
   a.n_own_chunks = (int)((own_keys + chunk - 1) / chunk);
@@ -618,23 +690,11 @@ size_t scored_workspace_most(const ScoredArgs& given, int sm_count) {
     const int tiles = (a.suffix_bound + a.T + SW_KEYS - 1) / SW_KEYS, most = 2 * sm_count / per_chunk;
     return sw_floats(a, (size_t)a.attn.n_prefix_chunks + (tiles < most ? tiles : (most > 1 ? most : 1)));
   }
-  // chunks grow with the bound, in a few steps, and within a step so does the need: the last bound of each step decides
-  size_t floats = 0;
-  for (int lo = 0; lo <= given.suffix_bound;) {
-    a.suffix_bound = lo;
-    const int chunk = sc_chunk(a, sm_count);
-    int x = lo, y = given.suffix_bound;
-    while (x < y) {
-      a.suffix_bound = x + (y - x + 1) / 2;
-      if (sc_chunk(a, sm_count) == chunk) x = a.suffix_bound; else y = a.suffix_bound - 1;
-    }
-    a.suffix_bound = x;
-    scored_plan(a, sm_count);
-    const size_t f = sc_floats(a);
-    floats = f > floats ? f : floats;
-    lo = x + 1;
-  }
-  return floats;
+  // a CTA writes 16 rows of partial results; there are never more than four waves of CTAs and one for each item, nor more than
+  // rounds of keys and one for each item (sc_chunk)
+  const long long items = (long long)a.Hkv * ((long long)a.n * a.rt_own + a.rt_prefix);
+  const long long waves = 4ll * sc_resident(a, sm_count), rounds = sc_work(a) / SC_KEYS + 1;
+  return (size_t)(16 * ((waves < rounds ? waves : rounds) + items)) * (a.hd + 2) + sc_rows(a) * ((size_t)a.ld_prefix + a.ld_own);
 }
 
 void scored_carve(ScoredArgs& a, float* ws) {              // ws: 16-byte aligned
@@ -657,14 +717,19 @@ void scored_carve(ScoredArgs& a, float* ws) {              // ws: 16-byte aligne
 template <int HD>
 static cudaError_t sc_launch(const ScoredArgs& a, cudaStream_t st) {
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)HD);
-  scored_rows_kernel<HD><<<dim3((unsigned)(a.n_prefix_chunks * a.rt_prefix + a.n * a.n_own_chunks * a.rt_own), (unsigned)a.Hkv), SC_WARPS * 32, 0, st>>>(a, scale_log2);
+  scored_rows_kernel<HD><<<dim3((unsigned)(a.n_prefix_chunks * a.rt_prefix + a.n * a.n_own_chunks * a.rt_own), (unsigned)a.Hkv), SC_WARPS * 32, ScCfg<HD>::SMEM, st>>>(a, scale_log2);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   const int out_blocks = (a.n * a.T * a.Hq + FIN_THREADS / 32 - 1) / (FIN_THREADS / 32);
-  const int prefix_blocks = a.prefix_weight != nullptr ? (a.P + FIN_THREADS - 1) / FIN_THREADS : 0;
-  const int own_blocks = (a.suffix_bound + a.T + FIN_THREADS - 1) / FIN_THREADS;
-  scored_finish_kernel<HD><<<out_blocks + a.Hkv * prefix_blocks + a.n * a.Hkv * own_blocks, FIN_THREADS, 0, st>>>(a, out_blocks, prefix_blocks, own_blocks);
-  return cudaGetLastError();
+  const int prefix_blocks = a.prefix_weight != nullptr ? (a.P + FIN_KEYS - 1) / FIN_KEYS : 0;
+  const int own_blocks = (a.suffix_bound + a.T + FIN_KEYS - 1) / FIN_KEYS;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(out_blocks + a.Hkv * prefix_blocks + a.n * a.Hkv * own_blocks)); cfg.blockDim = dim3(FIN_THREADS); cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, scored_finish_kernel<HD>, a, out_blocks, prefix_blocks, own_blocks);
 }
 
 cudaError_t launch_attention_scored(const ScoredArgs& a, cudaStream_t st) {

@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(THREADS) kv_select_kernel(const EvictArgs p, c
     if (tid == 0 && blockIdx.x == 0) atomicCAS(p.status, 0, MLORA_ERR_ARG);
     S = S < 0 ? 0 : p.bound;
   }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (!move_here) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (kv_move_kernel, which waits for this one)
   const int B = p.budget;
   if (tid == 0 && blockIdx.x == 0) p.out_len[s] = min(S, B);
   int2* const list = p.moves + (size_t)pair * p.max_moves;

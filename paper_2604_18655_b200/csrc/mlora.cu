@@ -2056,7 +2056,7 @@ static ScoredArgs scored_fill(int n, int T, int Hq, int Hkv, int hd, int P, int 
 
 static bool scored_shape(int32_t n, int32_t T, int32_t Hq, int32_t Hkv, int32_t P, int32_t suffix_bound) {
   return n > 0 && T > 0 && T <= 64 && Hq > 0 && Hkv > 0 && Hkv <= 65535 && Hq % Hkv == 0 && P >= 0 && suffix_bound >= 0 &&
-         P < (1 << 30) && suffix_bound < (1 << 30) && (long long)n * T * Hq < (1ll << 30);
+         P < (1 << 28) && suffix_bound < (1 << 28) && (long long)n * T * Hq < (1ll << 30);
 }
 
 size_t mlora_attention_scored_workspace_bytes(int32_t n, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, int32_t P,
