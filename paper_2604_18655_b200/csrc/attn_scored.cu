@@ -259,8 +259,9 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
   }
 }
 
-constexpr int FIN_THREADS = 128, FIN_KEYS = 4 * FIN_THREADS;
-constexpr int FIN_ROWS = 256;                              // rows whose maximum and 1 / sum are held at a time
+constexpr int FIN_THREADS = 128, FIN_KEYS = 128;
+constexpr int FIN_ROWS = 512;                              // rows whose maximum and 1 / sum are held at a time
+constexpr int FIN_FLY = 8;                                 // reads of a thread on their way at a time
 
 __device__ __forceinline__ int sc_len(const ScoredArgs& p, int s) {
   const int S = p.suffix_len[s];
@@ -271,79 +272,107 @@ __device__ __forceinline__ int sc_slots(const ScoredArgs& p, int s) {
   return p.n_prefix_chunks + min(p.n_own_chunks, (sc_len(p, s) + p.T + p.own_chunk - 1) / p.own_chunk);
 }
 
-// Blocks: rows of the output (one warp a row), then the prefix keys (four a thread), then the own keys.  A row's chunks are joined
-// by several lanes at once: one read's latency for all of them.
+// One warp: row w = kv head * R_all + v joined from its slots and written; returns (maximum, 1 / sum).  ns(s): slots that a row of
+// stream s has.
+template <int HD, class F>
+__device__ __forceinline__ float2 sc_join_row(const ScoredArgs& p, int w, int R_all, int slots, int lane, F&& slots_of) {
+  constexpr int N = HD / 32;                               // features of a lane
+  const int G = p.Hq / p.Hkv, kh = w / R_all, v = w - kh * R_all, m = v / G;
+  const size_t at = (size_t)w * slots;
+  const float2* const ml_at = reinterpret_cast<const float2*>(p.part_ml) + at;
+  float M = -INFINITY, L = 0.f, a[N] = {};
+  int ns = slots;
+  for (int i0 = 0; i0 < ns; i0 += FIN_FLY) {               // FIN_FLY slots at a time, in order
+    float x[FIN_FLY][N];
+    float2 ml[FIN_FLY];
+#pragma unroll
+    for (int i = 0; i < FIN_FLY; ++i) {
+      const int k = i0 + i;
+      ml[i] = make_float2(-INFINITY, 0.f);
+      if (k >= slots) continue;
+      asm volatile("ld.global.cg.v2.f32 {%0, %1}, [%2];" : "=f"(ml[i].x), "=f"(ml[i].y) : "l"(ml_at + k) : "memory");
+      const float* po = p.part_o + (at + k) * HD + lane * N;
+      if constexpr (N == 4) asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[i][0]), "=f"(x[i][1]), "=f"(x[i][2]), "=f"(x[i][3]) : "l"(po) : "memory");
+      else asm volatile("ld.global.cg.v2.f32 {%0, %1}, [%2];" : "=f"(x[i][0]), "=f"(x[i][1]) : "l"(po) : "memory");
+    }
+    if (i0 == 0) ns = slots_of(m / p.T);
+    float Mn = M;
+#pragma unroll
+    for (int i = 0; i < FIN_FLY; ++i) Mn = i0 + i < ns ? fmaxf(Mn, ml[i].x) : Mn;
+    const float Mb = Mn == -INFINITY ? 0.f : Mn, f0 = sc_ex2(M - Mb);
+    M = Mn;
+    L *= f0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) a[j] *= f0;
+#pragma unroll
+    for (int i = 0; i < FIN_FLY; ++i)
+      if (i0 + i < ns) {
+        const float f = sc_ex2(ml[i].x - Mb);
+        L = fmaf(f, ml[i].y, L);
+#pragma unroll
+        for (int j = 0; j < N; ++j) a[j] = fmaf(f, x[i][j], a[j]);
+      }
+  }
+  const float inv = 1.f / L;
+  __half2* dst = reinterpret_cast<__half2*>(p.out + ((size_t)m * p.Hq + kh * G + (v - m * G)) * HD + lane * N);
+#pragma unroll
+  for (int j = 0; j < N / 2; ++j) dst[j] = __floats2half2_rn(a[2 * j] * inv, a[2 * j + 1] * inv);
+  return make_float2(M == -INFINITY ? 0.f : M, inv);
+}
+
+// Blocks: rows of the output (one warp a row), then the prefix keys (a lane has four keys; a warp all rows of up to eight, else every
+// fourth row of the block's 128 keys), then the own keys.  Bound by the length of its chain of reads, so everything whose address is known goes out first: partial results
+// and scores before the length, maxima and sums that say what they count for (memory of the workspace in any case, never written
+// in vain).  A row's chunks are joined by several lanes at once.
 template <int HD>
 __global__ void __launch_bounds__(FIN_THREADS) scored_finish_kernel(const ScoredArgs p, const int out_blocks, const int prefix_blocks, const int own_blocks) {
   __shared__ float2 row_s[FIN_ROWS];
-  const int tid = threadIdx.x, lane = tid & 31, G = p.Hq / p.Hkv, R = p.T * G, R_all = p.n * R, slots = p.n_prefix_chunks + p.n_own_chunks;
+  __shared__ __align__(16) float sum_s[FIN_THREADS / 32][FIN_KEYS];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = p.Hq / p.Hkv, R = p.T * G, R_all = p.n * R, slots = p.n_prefix_chunks + p.n_own_chunks;
   const float2* const ml_all = reinterpret_cast<const float2*>(p.part_ml);
   int b = blockIdx.x;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
   if (b < out_blocks) {
-    constexpr int F = HD / 32;                             // features of a lane
-    const int w = b * (FIN_THREADS / 32) + (tid >> 5);
+    const int w = b * (FIN_THREADS / 32) + warp;
     if (w >= p.Hkv * R_all) return;
-    const int kh = w / R_all, v = w - kh * R_all, m = v / G, ns = sc_slots(p, m / p.T);
-    const size_t at = (size_t)w * slots;
-    float M = -INFINITY, L = 0.f, a[F] = {};
-    for (int i0 = 0; i0 < ns; i0 += 32) {                  // 32 slots at a time, in order
-      const float2 ml = i0 + lane < ns ? __ldcg(ml_all + at + i0 + lane) : make_float2(-INFINITY, 0.f);
-      float x = ml.x;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-      const float Mn = fmaxf(M, x), Mb = Mn == -INFINITY ? 0.f : Mn, f0 = sc_ex2(M - Mb), fl = sc_ex2(ml.x - Mb);
-      M = Mn;
-      L = L * f0 + warp_sum(fl * ml.y);
-#pragma unroll
-      for (int j = 0; j < F; ++j) a[j] *= f0;
-      const int n = min(32, ns - i0);
-      const float* po = p.part_o + (at + i0) * HD + lane * F;
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) {
-        const float f = __shfl_sync(0xffffffffu, fl, i);
-        if constexpr (F == 4) {
-          const float4 x4 = __ldcg(reinterpret_cast<const float4*>(po + (size_t)i * HD));
-          a[0] = fmaf(f, x4.x, a[0]); a[1] = fmaf(f, x4.y, a[1]); a[2] = fmaf(f, x4.z, a[2]); a[3] = fmaf(f, x4.w, a[3]);
-        } else {
-          const float2 x2 = __ldcg(reinterpret_cast<const float2*>(po + (size_t)i * HD));
-          a[0] = fmaf(f, x2.x, a[0]); a[1] = fmaf(f, x2.y, a[1]);
-        }
-      }
-    }
-    const float inv = 1.f / L;
-    __half2* dst = reinterpret_cast<__half2*>(p.out + ((size_t)m * p.Hq + kh * G + (v - m * G)) * HD + lane * F);
-#pragma unroll
-    for (int j = 0; j < F / 2; ++j) dst[j] = __floats2half2_rn(a[2 * j] * inv, a[2 * j + 1] * inv);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    sc_join_row<HD>(p, w, R_all, slots, lane, [&](int s) { return sc_slots(p, s); });
     return;
   }
   b -= out_blocks;
-  int kh, s = 0, key, v0, v1, ld, limit;
+  const bool own = b >= p.Hkv * prefix_blocks;
+  int kh, s = 0, key0, step, v0, v1, ld, limit;            // the block's 128 keys from key0 on, then those `step` keys on, ...
   const float* sc;
   float* dst;
-  if (b < p.Hkv * prefix_blocks) {
-    kh = b / prefix_blocks; key = (b - kh * prefix_blocks) * FIN_KEYS + 4 * tid;
+  if (!own) {
+    kh = b / prefix_blocks; key0 = (b - kh * prefix_blocks) * FIN_KEYS; step = prefix_blocks * FIN_KEYS;
     v0 = 0; v1 = R_all; ld = p.ld_prefix; sc = p.sc_prefix; limit = p.P;
     dst = p.prefix_weight + (size_t)kh * p.P;
   } else {
     b -= p.Hkv * prefix_blocks;
     const int seg = b / own_blocks;
-    kh = seg % p.Hkv; s = seg / p.Hkv; key = (b - seg * own_blocks) * FIN_KEYS + 4 * tid;
+    kh = seg % p.Hkv; s = seg / p.Hkv; key0 = (b - seg * own_blocks) * FIN_KEYS; step = own_blocks * FIN_KEYS;
     v0 = s * R; v1 = v0 + R; ld = p.ld_own; sc = p.sc_own;
-    limit = sc_len(p, s) + p.T;
-    if (key - 4 * tid >= limit) return;
     dst = p.own_weight + ((size_t)s * p.Hkv + kh) * p.cap;
+    limit = sc_len(p, s) + p.T;
+    if (key0 >= limit) return;
   }
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int r0 = v0; r0 < v1; r0 += FIN_ROWS) {
-    const int rows = min(FIN_ROWS, v1 - r0);
-    __syncthreads();
-    for (int r = tid >> 3; r < ((rows + 15) & ~15); r += FIN_THREADS / 8) {      // eight lanes a row
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  float4 x[FIN_FLY];
+  const int r_step = v1 - v0 <= FIN_FLY ? 1 : 4;
+  auto fetch = [&](int k0, int r0, int rows, int r) {      // keys k0 + 4 lane ... of rows r0 + r, r0 + r + r_step, ...
+    const float* const at = sc + ((size_t)kh * R_all + r0) * ld + min(k0 + 4 * lane, ld - 4);   // (a scratch row is a multiple of 16 keys)
+#pragma unroll
+    for (int i = 0; i < FIN_FLY; ++i)
+      if (r + i * r_step < rows)
+        asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[i].x), "=f"(x[i].y), "=f"(x[i].z), "=f"(x[i].w) : "l"(at + (size_t)(r + i * r_step) * ld) : "memory");
+  };
+  auto normalisers = [&](int r0, int rows) {               // eight lanes a row
+    for (int r = tid >> 3; r < ((rows + 15) & ~15); r += FIN_THREADS / 8) {
       const int v = r0 + min(r, rows - 1), ns = sc_slots(p, v / R), l = lane & 7;
-      const float2* const at = ml_all + ((size_t)kh * R_all + v) * slots;
+      const float2* const ml_at = ml_all + ((size_t)kh * R_all + v) * slots;
       float M = -INFINITY, L = 0.f;
       for (int i = l; i < ns; i += 8) {
-        const float2 ml = __ldcg(at + i);
+        const float2 ml = __ldcg(ml_at + i);
         const float Mn = fmaxf(M, ml.x), Mb = Mn == -INFINITY ? 0.f : Mn;
         L = L * sc_ex2(M - Mb) + ml.y * sc_ex2(ml.x - Mb);
         M = Mn;
@@ -357,76 +386,126 @@ __global__ void __launch_bounds__(FIN_THREADS) scored_finish_kernel(const Scored
       }
       if (l == 0 && r < rows) row_s[r] = make_float2(M == -INFINITY ? 0.f : M, 1.f / L);
     }
+  };
+  if (v1 - v0 <= FIN_FLY) {
+    // few rows: every warp takes 128 keys of its own, all rows at once
+    const int rows = v1 - v0;
+    key0 += (key0 / FIN_KEYS * 3 + warp) * FIN_KEYS;       // (block i: keys 512 i ...)
+    step *= 4;
+    fetch(key0, v0, rows, 0);
+    normalisers(v0, rows);
     __syncthreads();
-    if (key < limit) {
-      const float* at = sc + ((size_t)kh * R_all + r0) * ld + key;
-#pragma unroll 4
-      for (int r = 0; r < rows; ++r) {
-        const float2 ml = row_s[r];
-        const float4 x = __ldcg(reinterpret_cast<const float4*>(at + (size_t)r * ld));
-        sum[0] = fmaf(sc_ex2(x.x - ml.x), ml.y, sum[0]); sum[1] = fmaf(sc_ex2(x.y - ml.x), ml.y, sum[1]);
-        sum[2] = fmaf(sc_ex2(x.z - ml.x), ml.y, sum[2]); sum[3] = fmaf(sc_ex2(x.w - ml.x), ml.y, sum[3]);
+    for (int k0 = key0; k0 < limit; k0 += step) {
+      const int k = k0 + 4 * lane;
+      if (k0 != key0) fetch(k0, v0, rows, 0);
+      float old[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) old[i] = k + i < limit ? dst[k + i] : 0.f;
+#pragma unroll
+      for (int i = 0; i < FIN_FLY; ++i)
+        if (i < rows) {
+          const float2 ml = row_s[i];
+          sum[0] = fmaf(sc_ex2(x[i].x - ml.x), ml.y, sum[0]); sum[1] = fmaf(sc_ex2(x[i].y - ml.x), ml.y, sum[1]);
+          sum[2] = fmaf(sc_ex2(x[i].z - ml.x), ml.y, sum[2]); sum[3] = fmaf(sc_ex2(x[i].w - ml.x), ml.y, sum[3]);
+        }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (k + i < limit) dst[k + i] = old[i] + sum[i];
+    }
+    return;
+  }
+  const bool once = v1 - v0 <= FIN_ROWS;                   // the rows' normalisers are made once
+  for (int k0 = key0; k0 < limit; k0 += step) {
+    const float old = k0 + tid < limit ? dst[k0 + tid] : 0.f;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int r0 = v0; r0 < v1; r0 += FIN_ROWS) {
+      const int rows = min(FIN_ROWS, v1 - r0);
+      fetch(k0, r0, rows, warp);
+      if (!once || k0 == key0) {
+        __syncthreads();
+        normalisers(r0, rows);
+        __syncthreads();
+      }
+      for (int r = warp; r < rows; r += 4 * FIN_FLY) {
+        if (r != warp) fetch(k0, r0, rows, r);
+#pragma unroll
+        for (int i = 0; i < FIN_FLY; ++i)
+          if (r + i * 4 < rows) {
+            const float2 ml = row_s[r + i * 4];
+            sum[0] = fmaf(sc_ex2(x[i].x - ml.x), ml.y, sum[0]); sum[1] = fmaf(sc_ex2(x[i].y - ml.x), ml.y, sum[1]);
+            sum[2] = fmaf(sc_ex2(x[i].z - ml.x), ml.y, sum[2]); sum[3] = fmaf(sc_ex2(x[i].w - ml.x), ml.y, sum[3]);
+          }
       }
     }
+    if (k0 != key0) __syncthreads();
+    *reinterpret_cast<float4*>(&sum_s[warp][4 * lane]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    __syncthreads();
+    if (k0 + tid < limit) dst[k0 + tid] = old + ((sum_s[0][tid] + sum_s[1][tid]) + (sum_s[2][tid] + sum_s[3][tid]));
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (key + i < limit) dst[key + i] += sum[i];
 }
 
 // ----------------------------------------------------------------------------- many rows a KV head (trees, wide groups)
-// Attention as mlora_attention runs it (attn_tc_kernel and its merge), whose partial maxima and sums then give every row's
-// normaliser; a second pass over K alone makes the scores again, on the tensor cores, and sums the weights key by key.  For 96 rows a
-// KV head the scores in scratch would be 768 bytes of traffic a key, K is 256.
-// One CTA: 128 keys of a segment against all rows that see them, up to 128 at a time.  S^T = K Q^T with the keys as the rows of
-// the accumulator: a thread owns a key (its tensor-memory lane), so that sums over query rows stay in the thread and no order of
-// work can change them.  Two accumulators: the next block's product is made while this one's exponentials are.
+// Attention as mlora_attention runs it (attn_tc_kernel), its partial results joined by scored_join_kernel, which leaves every row's
+// maximum and 1 / sum; a second pass over K alone makes the scores again, on the tensor cores, and sums the weights key by key.  For
+// 96 rows a KV head the scores in scratch would be 768 bytes of traffic a key, K is 256.
+// scored_weights_kernel: 128 keys of a segment against up to 128 of the rows that see them at a time.  S^T = K Q^T with the keys as
+// the rows of the accumulator: a thread owns a key (its tensor-memory lane), so that sums over query rows stay in the thread and no
+// order of work can change them.  A CTA keeps one operand and streams the other: a tile of prefix keys against all blocks of rows,
+// or a stream's rows (where they are one block) against several tiles of its own keys.  Two accumulators: the next product is made
+// while this one's exponentials are.
 // What bounds it: the exponentials, 8 clocks an SM for a row of a tile (16 a clock).
-constexpr int SW_KEYS = 128, SW_ROWS = 128, SW_SLOTS = 8, SW_THREADS = 160;
+constexpr int SW_KEYS = 128, SW_ROWS = 128, SW_THREADS = 160;
 template <int HD> struct SwCfg {
   static constexpr uint32_t TILE = SW_KEYS * HD * 2;
   static constexpr size_t SMEM = 3 * (size_t)TILE + 1024;
 };
 
-// the row's normaliser from its chunks' maxima and sums: (maximum, 1 / sum)
-__device__ __forceinline__ float2 sw_join(const float2* ml, int ns) {
-  float M = -INFINITY, L = 0.f;
-  for (int i = 0; i < ns; ++i) M = fmaxf(M, __ldcg(ml + i).x);
-  const float Mb = M == -INFINITY ? 0.f : M;
-  for (int i = 0; i < ns; ++i) { const float2 x = __ldcg(ml + i); L += sc_ex2(x.x - Mb) * x.y; }
-  return make_float2(Mb, 1.f / L);
+template <int HD>
+__global__ void __launch_bounds__(FIN_THREADS) scored_join_kernel(const ScoredArgs p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // (scored_weights_kernel, which waits for this one)
+  const int w = blockIdx.x * (FIN_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31, R_all = p.n * p.T * (p.Hq / p.Hkv);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (w >= p.Hkv * R_all) return;
+  const AttnArgs& t = p.attn;
+  const float2 ml = sc_join_row<HD>(p, w, R_all, t.n_prefix_chunks + t.n_own_chunks, lane, [&](int s) {
+    return t.n_prefix_chunks + min(t.n_own_chunks, (p.lens[s] + p.T + t.own_chunk - 1) / t.own_chunk); });
+  if (lane == 0) p.row_ml[w] = ml;
 }
 
 template <int HD>
 __global__ void __launch_bounds__(SW_THREADS, 2)
-scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const int prefix_tiles, const int own_tiles, const float scale_log2,
+scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const int prefix_tiles, const int own_ctas, const int own_per, const float scale_log2,
                       const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_pk, const __grid_constant__ CUtensorMap map_ok) {
   constexpr int HALVES = HD / 64;
   constexpr uint32_t TILE = SwCfg<HD>::TILE, HALF = SW_KEYS * 128;
   extern __shared__ __align__(1024) unsigned char sw_smem[];
-  __shared__ __align__(8) uint64_t k_full, q_full[2], q_empty[2], s_full[2], s_empty[2];
+  __shared__ __align__(8) uint64_t fix_full, mov_full[2], mov_empty[2], s_full[2], s_empty[2];
   __shared__ __align__(16) float2 ml_s[2][SW_ROWS];
   __shared__ unsigned long long anc_s[2][SW_ROWS];
   __shared__ uint32_t tmem_s;
-  const uint32_t k_sm = (tc_smem_u32(sw_smem) + 1023u) & ~1023u, q_sm = k_sm + TILE;
+  const uint32_t fix_sm = (tc_smem_u32(sw_smem) + 1023u) & ~1023u, mov_sm = fix_sm + TILE;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  const int kh = blockIdx.y, G = p.Hq / p.Hkv, R = p.T * G, R_all = p.n * R, slots = p.attn.n_prefix_chunks + p.attn.n_own_chunks;
+  const int kh = blockIdx.y, G = p.Hq / p.Hkv, R = p.T * G, R_all = p.n * R;
   const bool own = (int)blockIdx.x >= prefix_tiles;
-  int s = 0, key0, limit, v_lo = 0, v_hi = R_all, S = 0;
-  if (own) asm volatile("griddepcontrol.wait;" ::: "memory");          // (the lengths are written by this call)
+  int s = 0, key0, limit, v_lo = 0, v_hi = R_all, S = 0, units;
+  bool mov_k = false;                                      // the keys are what moves
   if (!own) {
     key0 = blockIdx.x * SW_KEYS; limit = p.P;
+    units = (R_all + rb - 1) / rb;
   } else {
+    // (the lengths are written by this call)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int i = blockIdx.x - prefix_tiles;
-    s = i / own_tiles; key0 = (i - s * own_tiles) * SW_KEYS;
+    s = i / own_ctas; key0 = (i - s * own_ctas) * own_per * SW_KEYS;
     S = p.lens[s]; limit = S + p.T;
     v_lo = s * R; v_hi = v_lo + R;
     if (key0 >= limit) return;
+    mov_k = R <= rb;                                       // (else own_per is 1)
+    units = mov_k ? min(own_per, (limit - key0 + SW_KEYS - 1) / SW_KEYS) : (R + rb - 1) / rb;
   }
-  const int blocks = (v_hi - v_lo + rb - 1) / rb;
   if (tid == 0) {
-    TC_MBAR_INIT(&k_full, 1);
-    for (int i = 0; i < 2; ++i) { TC_MBAR_INIT(q_full + i, 1); TC_MBAR_INIT(q_empty + i, 1); TC_MBAR_INIT(s_full + i, 1); TC_MBAR_INIT(s_empty + i, 4); }
+    TC_MBAR_INIT(&fix_full, 1);
+    for (int i = 0; i < 2; ++i) { TC_MBAR_INIT(mov_full + i, 1); TC_MBAR_INIT(mov_empty + i, 1); TC_MBAR_INIT(s_full + i, 1); TC_MBAR_INIT(s_empty + i, 4); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 4) {
@@ -440,79 +519,91 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
   if (warp == 4) {
     // ---- copies and MMAs, by one thread.  Neither K nor q is written by the kernels of this call.
     if (tc_elect()) {
-      auto load_q = [&](int b) {
-        const uint32_t bar = tc_smem_u32(q_full + (b & 1)), dst = q_sm + (b & 1) * TILE;
+      auto load_q = [&](uint32_t dst, int b, uint32_t bar) {
         tc_expect_tx(bar, HALVES * (uint32_t)rb * 128u);
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) at_copy3(dst + h * HALF, &map_q, h * 64, kh * G, (v_lo + b * rb) / G, bar);
       };
-      tc_expect_tx(tc_smem_u32(&k_full), TILE);
+      auto load_k = [&](uint32_t dst, int i, uint32_t bar) {
+        tc_expect_tx(bar, TILE);
 #pragma unroll
-      for (int h = 0; h < HALVES; ++h) {
-        if (own) at_copy4(k_sm + h * HALF, &map_ok, h * 64, key0, kh, s, tc_smem_u32(&k_full));
-        else at_copy3(k_sm + h * HALF, &map_pk, h * 64, key0, kh, tc_smem_u32(&k_full));
-      }
-      load_q(0);
-      if (blocks > 1) load_q(1);
+        for (int h = 0; h < HALVES; ++h) {
+          if (own) at_copy4(dst + h * HALF, &map_ok, h * 64, key0 + i * SW_KEYS, kh, s, bar);
+          else at_copy3(dst + h * HALF, &map_pk, h * 64, key0 + i * SW_KEYS, kh, bar);
+        }
+      };
+      auto load = [&](int u) {
+        const uint32_t bar = tc_smem_u32(mov_full + (u & 1)), dst = mov_sm + (u & 1) * TILE;
+        if (mov_k) load_k(dst, u, bar); else load_q(dst, u, bar);
+      };
+      if (mov_k) load_q(fix_sm, 0, tc_smem_u32(&fix_full)); else load_k(fix_sm, 0, tc_smem_u32(&fix_full));
+      load(0);
+      if (units > 1) load(1);
       constexpr uint64_t DESC = ((uint64_t)1 << 46) | ((uint64_t)2 << 61) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 16);
       auto desc = [](uint32_t a) { return DESC | (uint64_t)((a & 0x3FFFF) >> 4); };
-      int loaded = blocks > 1 ? 2 : 1;
-      bool alive = tc_wait(tc_smem_u32(&k_full), 0u, p.status);
-      for (int b = 0; b < blocks && alive; ++b) {
-        const int st = b & 1; const uint32_t ph = (uint32_t)((b >> 1) & 1);
-        alive = tc_wait(tc_smem_u32(q_full + st), ph, p.status) && tc_wait(tc_smem_u32(s_empty + st), ph ^ 1u, p.status);
+      int loaded = units > 1 ? 2 : 1;
+      bool alive = tc_wait(tc_smem_u32(&fix_full), 0u, p.status);
+      for (int u = 0; u < units && alive; ++u) {
+        const int st = u & 1; const uint32_t ph = (uint32_t)((u >> 1) & 1);
+        alive = tc_wait(tc_smem_u32(mov_full + st), ph, p.status) && tc_wait(tc_smem_u32(s_empty + st), ph ^ 1u, p.status);
         if (!alive) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const int n_rows = min(rb, v_hi - v_lo - b * rb);
+        const int n_rows = mov_k ? R : min(rb, v_hi - v_lo - u * rb);
         const uint32_t idesc = (1u << 4) | ((uint32_t)((n_rows + 15) / 16 * 2) << 17) | ((SW_KEYS >> 4) << 24);
+        const uint32_t mov = mov_sm + st * TILE, k_sm = mov_k ? mov : fix_sm, q_sm = mov_k ? fix_sm : mov;
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) {
           const uint32_t off = (kk >> 2) * HALF + (kk & 3) * 32;
           asm volatile(
               "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
               "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-              ::"r"(tmem + st * 128), "l"(desc(k_sm + off)), "l"(desc(q_sm + st * TILE + off)), "r"(idesc), "r"(kk > 0 ? 1u : 0u) : "memory");
+              ::"r"(tmem + st * 128), "l"(desc(k_sm + off)), "l"(desc(q_sm + off)), "r"(idesc), "r"(kk > 0 ? 1u : 0u) : "memory");
         }
         tc_commit(tc_smem_u32(s_full + st));
-        tc_commit(tc_smem_u32(q_empty + st));
-        if (b + 2 < blocks) {
-          alive = tc_wait(tc_smem_u32(q_empty + st), ph, p.status);
-          if (alive) { load_q(b + 2); loaded = b + 3; }
+        tc_commit(tc_smem_u32(mov_empty + st));
+        if (u + 2 < units) {
+          alive = tc_wait(tc_smem_u32(mov_empty + st), ph, p.status);
+          if (alive) { load(u + 2); loaded = u + 3; }
         }
       }
       // no copy may be in flight when the CTA ends (passes at once unless a wait gave up somewhere)
       if (!alive) {
-        tc_wait(tc_smem_u32(&k_full), 0u, p.status);
-        for (int b = loaded > 2 ? loaded - 2 : 0; b < loaded; ++b) tc_wait(tc_smem_u32(q_full + (b & 1)), (uint32_t)((b >> 1) & 1), p.status);
+        tc_wait(tc_smem_u32(&fix_full), 0u, p.status);
+        for (int u = loaded > 2 ? loaded - 2 : 0; u < loaded; ++u) tc_wait(tc_smem_u32(mov_full + (u & 1)), (uint32_t)((u >> 1) & 1), p.status);
       }
     }
     __syncwarp();
   } else {
-    // ---- weights: thread = key; a block's rows' normalisers are brought by the same threads, one row each
+    // ---- weights: thread = key; a block's rows' normalisers are brought by the same threads, one row each, a unit ahead
     if (!own) asm volatile("griddepcontrol.wait;" ::: "memory");
-    const float2* const ml_all = reinterpret_cast<const float2*>(p.part_ml) + (size_t)kh * R_all * slots;
-    auto slots_of = [&](int v) { return p.attn.n_prefix_chunks + min(p.attn.n_own_chunks, (p.lens[v / R] + p.T + p.attn.own_chunk - 1) / p.attn.own_chunk); };
-    const int key = key0 + tid, d = key - S;
-    const bool masked = own && key0 + SW_KEYS > S && p.T > 1;          // (the same for the whole CTA)
+    float* const dst = own ? p.own_weight + ((size_t)s * p.Hkv + kh) * p.cap : p.prefix_weight + (size_t)kh * p.P;
+    const bool tree = own && p.T > 1;
     bool alive = true;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
     float2 next = make_float2(0.f, 0.f);
     unsigned long long next_anc = 0ull;
     auto fetch = [&](int b) {
       const int v = v_lo + b * rb + tid;
-      if (tid < rb && v < v_hi) { next = sw_join(ml_all + (size_t)v * slots, slots_of(v)); if (masked) next_anc = p.anc[v / G]; }
+      if (tid < rb && v < v_hi) {
+        asm volatile("ld.global.cg.v2.f32 {%0, %1}, [%2];" : "=f"(next.x), "=f"(next.y) : "l"(p.row_ml + (size_t)kh * R_all + v) : "memory");
+        if (tree) next_anc = p.anc[v / G];
+      }
     };
     fetch(0);
-    for (int b = 0; b < blocks; ++b) {
-      const int st = b & 1; const uint32_t ph = (uint32_t)((b >> 1) & 1);
-      ml_s[st][tid] = next;
-      if (masked) anc_s[st][tid] = next_anc;
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-      if (b + 1 < blocks) fetch(b + 1);
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < units; ++u) {
+      const int st = u & 1, ms = mov_k ? 0 : st; const uint32_t ph = (uint32_t)((u >> 1) & 1);
+      if (!mov_k || u == 0) {
+        ml_s[ms][tid] = next;
+        if (tree) anc_s[ms][tid] = next_anc;
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (!mov_k && u + 1 < units) fetch(u + 1);
+      }
+      const int tile0 = mov_k ? key0 + u * SW_KEYS : key0, key = tile0 + tid, d = key - S;
+      const bool masked = tree && tile0 + SW_KEYS > S;                 // (the same for the whole CTA)
       if (alive) alive = tc_wait(tc_smem_u32(s_full + st), ph, p.status);
       alive = __all_sync(0xffffffffu, alive);                          // (no way out: the other warps wait at the barrier)
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const int n_rows = alive ? min(rb, v_hi - v_lo - b * rb) : 0;
+      const int n_rows = !alive ? 0 : mov_k ? R : min(rb, v_hi - v_lo - u * rb);
       const uint32_t at = tmem + st * 128 + ((uint32_t)(warp * 32) << 16);
       for (int c0 = 0; c0 < n_rows; c0 += 32) {
         float x[32];
@@ -521,7 +612,7 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
         if (c0 + 32 <= n_rows && !masked) {
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
-            const float4 ml = *reinterpret_cast<const float4*>(&ml_s[st][c0 + i]);
+            const float4 ml = *reinterpret_cast<const float4*>(&ml_s[ms][c0 + i]);
             sum[i & 3] = fmaf(sc_ex2(fmaf(x[i], scale_log2, -ml.x)), ml.y, sum[i & 3]);
             sum[(i + 1) & 3] = fmaf(sc_ex2(fmaf(x[i + 1], scale_log2, -ml.z)), ml.w, sum[(i + 1) & 3]);
           }
@@ -529,8 +620,8 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             if (c0 + i < n_rows) {
-              const float2 ml = ml_s[st][c0 + i];
-              const bool see = !masked || d < 0 || (d < 64 && ((anc_s[st][c0 + i] >> d) & 1ull));
+              const float2 ml = ml_s[ms][c0 + i];
+              const bool see = !masked || d < 0 || (d < 64 && ((anc_s[ms][c0 + i] >> d) & 1ull));
               if (see) sum[i & 3] = fmaf(sc_ex2(fmaf(x[i], scale_log2, -ml.x)), ml.y, sum[i & 3]);
             }
           }
@@ -539,10 +630,8 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) tc_arrive(tc_smem_u32(s_empty + st));
-    }
-    if (alive && key < limit) {
-      float* dst = own ? p.own_weight + ((size_t)s * p.Hkv + kh) * p.cap : p.prefix_weight + (size_t)kh * p.P;
-      dst[key] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      if ((mov_k || u + 1 == units) && alive && key < limit) dst[key] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      if (mov_k) sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
     }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -589,8 +678,13 @@ static cudaError_t sw_launch(const ScoredArgs& a, cudaStream_t st) {
   t.own_k = a.own_k; t.own_v = a.own_v; t.own_head_stride = (size_t)a.cap * HD; t.own_stream_stride = t.own_head_stride * a.Hkv;
   t.suffix_len = a.lens; t.anc = a.anc; t.depth = a.depth; t.out = a.out; t.status = a.status; t.part_o = a.part_o; t.part_ml = a.part_ml;
   if ((e = launch_attention(t, st)) != cudaSuccess) return e;
-  t.pdl = 1;
-  if ((e = launch_attention_merge(t, st)) != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = st;
+  cfg.gridDim = dim3((unsigned)((rows * a.Hq + FIN_THREADS / 32 - 1) / (FIN_THREADS / 32))); cfg.blockDim = dim3(FIN_THREADS);
+  if ((e = cudaLaunchKernelEx(&cfg, scored_join_kernel<HD>, a)) != cudaSuccess) return e;
   const cuuint64_t H = sizeof(__half);
   CUtensorMap mq, mpk, mok;
   {
@@ -610,14 +704,14 @@ static cudaError_t sw_launch(const ScoredArgs& a, cudaStream_t st) {
     if ((e = at_map(a.own_k, 4, d, s, b, &mok)) != cudaSuccess) return e;
   }
   const int prefix_tiles = a.prefix_weight != nullptr ? (a.P + SW_KEYS - 1) / SW_KEYS : 0, own_tiles = (a.suffix_bound + a.T + SW_KEYS - 1) / SW_KEYS;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(prefix_tiles + a.n * own_tiles), (unsigned)a.Hkv);
-  cfg.blockDim = dim3(SW_THREADS); cfg.dynamicSmemBytes = SwCfg<HD>::SMEM; cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, scored_weights_kernel<HD>, a, rb, prefix_tiles, own_tiles, 1.4426950408889634f / sqrtf((float)HD), mq, mpk, mok);
+  // tiles of own keys that a CTA takes in turn: for two CTAs an SM in all, up to eight
+  const int room = 2 * 148 - a.Hkv * prefix_tiles, all = a.n * a.Hkv * own_tiles;
+  int own_per = (all + (room > 148 ? room : 148) - 1) / (room > 148 ? room : 148);
+  own_per = a.T * G > rb ? 1 : (own_per > 8 ? 8 : own_per);
+  const int own_ctas = (own_tiles + own_per - 1) / own_per;
+  cfg.gridDim = dim3((unsigned)(prefix_tiles + a.n * own_ctas), (unsigned)a.Hkv);
+  cfg.blockDim = dim3(SW_THREADS); cfg.dynamicSmemBytes = SwCfg<HD>::SMEM;
+  return cudaLaunchKernelEx(&cfg, scored_weights_kernel<HD>, a, rb, prefix_tiles, own_ctas, own_per, 1.4426950408889634f / sqrtf((float)HD), mq, mpk, mok);
 }
 
 cudaError_t init_scored() {
@@ -672,8 +766,8 @@ void scored_plan(ScoredArgs& a, int sm_count) {
 }
 
 static size_t sc_rows(const ScoredArgs& a) { return (size_t)a.n * a.T * a.Hq; }
-// tcgen05 form, behind the partial results: masks (two floats a node), lengths and depths
-static size_t sw_floats(const ScoredArgs& a, size_t slots) { return sc_rows(a) * slots * (a.hd + 2) + ((size_t)a.n * a.T + 1) * 4 + a.n; }
+// tcgen05 form, behind the partial results: the rows' normalisers, masks (two floats a node), depths and lengths
+static size_t sw_floats(const ScoredArgs& a, size_t slots) { return sc_rows(a) * slots * (a.hd + 2) + sc_rows(a) * 2 + ((size_t)a.n * a.T + 1) * 4 + a.n; }
 static size_t sc_floats(const ScoredArgs& a) {
   return sc_rows(a) * ((size_t)(a.n_prefix_chunks + a.n_own_chunks) * (a.hd + 2) + (size_t)a.ld_prefix + a.ld_own);
 }
@@ -703,7 +797,8 @@ void scored_carve(ScoredArgs& a, float* ws) {              // ws: 16-byte aligne
     const size_t parts = sc_rows(a) * ((size_t)a.attn.n_prefix_chunks + a.attn.n_own_chunks);
     a.part_ml = ws + parts * a.hd;
     float* const at = a.part_ml + (parts * 2 + 3) / 4 * 4;
-    a.anc = (unsigned long long*)at;
+    a.row_ml = (float2*)at;
+    a.anc = (unsigned long long*)(a.row_ml + sc_rows(a));
     a.depth = (int32_t*)(a.anc + (size_t)a.n * a.T);
     a.lens = a.depth + (size_t)a.n * a.T;
     return;
@@ -721,8 +816,14 @@ static cudaError_t sc_launch(const ScoredArgs& a, cudaStream_t st) {
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   const int out_blocks = (a.n * a.T * a.Hq + FIN_THREADS / 32 - 1) / (FIN_THREADS / 32);
-  const int prefix_blocks = a.prefix_weight != nullptr ? (a.P + FIN_KEYS - 1) / FIN_KEYS : 0;
-  const int own_blocks = (a.suffix_bound + a.T + FIN_KEYS - 1) / FIN_KEYS;
+  // (long segments: a block for every 128 keys only as far as that fills the machine, the rest in turns)
+  auto blocks_of = [](long long keys, long long segments, int rows) {
+    const int per = rows <= FIN_FLY ? 4 * FIN_KEYS : FIN_KEYS;
+    const long long all = (keys + per - 1) / per, fill = (148 * 16 + segments - 1) / segments;
+    return (int)(all < fill ? all : fill);
+  };
+  const int prefix_blocks = a.prefix_weight != nullptr ? blocks_of(a.P, a.Hkv, a.n * a.T * (a.Hq / a.Hkv)) : 0;
+  const int own_blocks = blocks_of((long long)a.suffix_bound + a.T, (long long)a.n * a.Hkv, a.T * (a.Hq / a.Hkv));
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(out_blocks + a.Hkv * prefix_blocks + a.n * a.Hkv * own_blocks)); cfg.blockDim = dim3(FIN_THREADS); cfg.stream = st;
   cudaLaunchAttribute attr[1];

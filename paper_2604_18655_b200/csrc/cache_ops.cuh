@@ -36,6 +36,7 @@ struct ScoredArgs {
   float *part_o, *part_ml, *sc_prefix, *sc_own;
   int tc;                               // many rows a KV head: the tcgen05 kernels
   AttnArgs attn;                        // ... their attention
+  float2* row_ml;                       // ... scratch: the rows' (maximum, 1 / sum)
   unsigned long long* anc;              // ... scratch: ancestor masks, clamped lengths, depths (not read)
   int32_t *lens, *depth;
 };
