@@ -583,6 +583,7 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
     unsigned long long next_anc = 0ull;
     auto fetch = [&](int b) {
       const int v = v_lo + b * rb + tid;
+      next = make_float2(0.f, 0.f);
       if (tid < rb && v < v_hi) {
         asm volatile("ld.global.cg.v2.f32 {%0, %1}, [%2];" : "=f"(next.x), "=f"(next.y) : "l"(p.row_ml + (size_t)kh * R_all + v) : "memory");
         if (tree) next_anc = p.anc[v / G];
@@ -605,27 +606,46 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const int n_rows = !alive ? 0 : mov_k ? R : min(rb, v_hi - v_lo - u * rb);
       const uint32_t at = tmem + st * 128 + ((uint32_t)(warp * 32) << 16);
-      for (int c0 = 0; c0 < n_rows; c0 += 32) {
-        float x[32];
-        at_ld32(at + c0, x);
+      // 32 columns at a time, the next ones on their way meanwhile; every step over all of them, so that no exponential waits for
+      // the one before (written one column after the other it took 45 clocks a column, eight times the exponential unit's)
+      float xs[2][32];
+      auto columns = [&](int c0, float (&x)[32], float (&following)[32]) {
         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        if (c0 + 32 <= n_rows && !masked) {
+        if (c0 + 32 < n_rows) at_ld32(at + c0 + 32, following);
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const float4 ml = *reinterpret_cast<const float4*>(&ml_s[ms][c0 + i]);
-            sum[i & 3] = fmaf(sc_ex2(fmaf(x[i], scale_log2, -ml.x)), ml.y, sum[i & 3]);
-            sum[(i + 1) & 3] = fmaf(sc_ex2(fmaf(x[i + 1], scale_log2, -ml.z)), ml.w, sum[(i + 1) & 3]);
-          }
-        } else {
+        for (int h = 0; h < 32; h += 16) {
+          float m[16], w[16];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            if (c0 + i < n_rows) {
-              const float2 ml = ml_s[ms][c0 + i];
-              const bool see = !masked || d < 0 || (d < 64 && ((anc_s[ms][c0 + i] >> d) & 1ull));
-              if (see) sum[i & 3] = fmaf(sc_ex2(fmaf(x[i], scale_log2, -ml.x)), ml.y, sum[i & 3]);
-            }
+          for (int i = 0; i < 16; i += 2) {
+            const float4 ml = *reinterpret_cast<const float4*>(&ml_s[ms][c0 + h + i]);
+            m[i] = ml.x; w[i] = ml.y; m[i + 1] = ml.z; w[i + 1] = ml.w;
           }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[h + i] = fmaf(x[h + i], scale_log2, -m[i]);
+          // rows past the end (whatever their accumulator columns hold) and nodes that do not see this key weigh nothing
+          if (c0 + 32 > n_rows) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[h + i] = c0 + h + i < n_rows ? x[h + i] : -INFINITY;
+          }
+          if (masked) {
+            const uint32_t* const words = reinterpret_cast<const uint32_t*>(&anc_s[ms][c0 + h]) + (d >= 32 ? 1 : 0);
+            const uint32_t always = d >= 0 ? 0u : 1u;
+            uint32_t see[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) see[i] = ((words[2 * i] >> (d & 31)) | always) & 1u;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[h + i] = see[i] ? x[h + i] : -INFINITY;
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[h + i] = sc_ex2(x[h + i]);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum[i & 3] = fmaf(x[h + i], w[i], sum[i & 3]);
         }
+      };
+      if (n_rows > 0) at_ld32(at, xs[0]);
+      for (int c0 = 0; c0 < n_rows; c0 += 64) {
+        columns(c0, xs[0], xs[1]);
+        if (c0 + 32 < n_rows) columns(c0 + 32, xs[1], xs[0]);
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
