@@ -452,7 +452,8 @@ __global__ void __launch_bounds__(FIN_THREADS) scored_finish_kernel(const Scored
 // the rows of the accumulator: a thread owns a key (its tensor-memory lane), so that sums over query rows stay in the thread and no
 // order of work can change them.  A CTA keeps one operand and streams the other: a tile of prefix keys against all blocks of rows,
 // or a stream's rows (where they are one block) against several tiles of its own keys.  Two accumulators: the next product is made
-// while this one's exponentials are.
+// while this one's exponentials are.  Many blocks of rows of a prefix tile are shared by a cluster of two CTAs, the second of which hands its
+// sums to the first.
 // What bounds it: the exponentials, 8 clocks an SM for a row of a tile (16 a clock).
 constexpr int SW_KEYS = 128, SW_ROWS = 128, SW_THREADS = 160;
 template <int HD> struct SwCfg {
@@ -474,7 +475,7 @@ __global__ void __launch_bounds__(FIN_THREADS) scored_join_kernel(const ScoredAr
 
 template <int HD>
 __global__ void __launch_bounds__(SW_THREADS, 2)
-scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const int prefix_tiles, const int own_ctas, const int own_per, const float scale_log2,
+scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const int prefix_ctas, const int pair, const int own_ctas, const int own_per, const float scale_log2,
                       const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_pk, const __grid_constant__ CUtensorMap map_ok) {
   constexpr int HALVES = HD / 64;
   constexpr uint32_t TILE = SwCfg<HD>::TILE, HALF = SW_KEYS * 128;
@@ -483,19 +484,26 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
   __shared__ __align__(16) float2 ml_s[2][SW_ROWS];
   __shared__ unsigned long long anc_s[2][SW_ROWS];
   __shared__ uint32_t tmem_s;
+  __shared__ float half_s[SW_KEYS];                        // the second CTA's sums
   const uint32_t fix_sm = (tc_smem_u32(sw_smem) + 1023u) & ~1023u, mov_sm = fix_sm + TILE;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int kh = blockIdx.y, G = p.Hq / p.Hkv, R = p.T * G, R_all = p.n * R;
-  const bool own = (int)blockIdx.x >= prefix_tiles;
+  const bool own = (int)blockIdx.x >= prefix_ctas, shared = pair && !own;
+  const int second = shared ? blockIdx.x & 1 : 0;          // (its rank in the cluster)
   int s = 0, key0, limit, v_lo = 0, v_hi = R_all, S = 0, units;
   bool mov_k = false;                                      // the keys are what moves
   if (!own) {
-    key0 = blockIdx.x * SW_KEYS; limit = p.P;
+    key0 = (blockIdx.x >> pair) * SW_KEYS; limit = p.P;
     units = (R_all + rb - 1) / rb;
+    if (shared) {
+      const int mine = (units + 1) / 2;
+      if (second) { v_lo = mine * rb; units -= mine; } else { units = mine; v_hi = min(R_all, mine * rb); }
+    }
   } else {
     // (the lengths are written by this call)
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int i = blockIdx.x - prefix_tiles;
+    const int i = blockIdx.x - prefix_ctas;
+    if (i >= p.n * own_ctas) return;                       // (the grid is made of whole clusters)
     s = i / own_ctas; key0 = (i - s * own_ctas) * own_per * SW_KEYS;
     S = p.lens[s]; limit = S + p.T;
     v_lo = s * R; v_hi = v_lo + R;
@@ -516,6 +524,8 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_s, 0);
+  float total = 0.f;
+  bool complete = false;
   if (warp == 4) {
     // ---- copies and MMAs, by one thread.  Neither K nor q is written by the kernels of this call.
     if (tc_elect()) {
@@ -650,11 +660,30 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) tc_arrive(tc_smem_u32(s_empty + st));
-      if ((mov_k || u + 1 == units) && alive && key < limit) dst[key] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      if (mov_k) sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
+      if (mov_k) {
+        if (alive && key < limit) dst[key] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
+      }
     }
+    if (!mov_k) {
+      total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      if (shared) half_s[tid] = total;
+      else if (alive && key0 + tid < limit) dst[key0 + tid] += total;
+    }
+    complete = alive;
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  if (shared) {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+    if (!second && warp < 4) {
+      uint32_t at;
+      float x;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(at) : "r"(tc_smem_u32(&half_s[tid])));
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+      if (complete && key0 + tid < limit) p.prefix_weight[(size_t)kh * p.P + key0 + tid] += total + x;
+    }
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");   // (read before its owner ends)
+  }
   __syncthreads();
   if (warp == 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
 }
@@ -699,7 +728,7 @@ static cudaError_t sw_launch(const ScoredArgs& a, cudaStream_t st) {
   t.suffix_len = a.lens; t.anc = a.anc; t.depth = a.depth; t.out = a.out; t.status = a.status; t.part_o = a.part_o; t.part_ml = a.part_ml;
   if ((e = launch_attention(t, st)) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = st;
@@ -724,14 +753,26 @@ static cudaError_t sw_launch(const ScoredArgs& a, cudaStream_t st) {
     if ((e = at_map(a.own_k, 4, d, s, b, &mok)) != cudaSuccess) return e;
   }
   const int prefix_tiles = a.prefix_weight != nullptr ? (a.P + SW_KEYS - 1) / SW_KEYS : 0, own_tiles = (a.suffix_bound + a.T + SW_KEYS - 1) / SW_KEYS;
-  // tiles of own keys that a CTA takes in turn: for two CTAs an SM in all, up to eight
-  const int room = 2 * 148 - a.Hkv * prefix_tiles, all = a.n * a.Hkv * own_tiles;
-  int own_per = (all + (room > 148 ? room : 148) - 1) / (room > 148 ? room : 148);
-  own_per = a.T * G > rb ? 1 : (own_per > 8 ? 8 : own_per);
-  const int own_ctas = (own_tiles + own_per - 1) / own_per;
-  cfg.gridDim = dim3((unsigned)(prefix_tiles + a.n * own_ctas), (unsigned)a.Hkv);
+  // Prefix tiles with several blocks of rows: one CTA each or two; own keys: so many tiles a CTA in turn.  By a CTA's time (a unit is 128
+  // keys by a block of rows, three units' worth of fixed cost) and the waves that all CTAs make, two an SM.  (8 x 32 nodes of llama3b
+  // heads: one wave of 7 and 5 units 17 us, two waves of 4 and 4 26.)
+  const int blocks = (rows * G + rb - 1) / rb;
+  int pair = 0, own_per = 1;
+  long long cost = -1;
+  for (int two = 0; two <= (prefix_tiles > 0 && blocks > 2 ? 1 : 0); ++two)
+    for (int per = 1; per <= (a.T * G > rb ? 1 : (own_tiles < 16 ? own_tiles : 16)); ++per) {
+      const long long ctas = (long long)a.Hkv * ((prefix_tiles << two) + a.n * ((own_tiles + per - 1) / per));
+      const int own_units = a.T * G > rb ? (a.T * G + rb - 1) / rb : per, prefix_units = prefix_tiles > 0 ? (blocks + two) >> two : 0;
+      const long long c = (ctas + 2 * 148 - 1) / (2 * 148) * (3 + (own_units > prefix_units ? own_units : prefix_units));
+      if (cost < 0 || c < cost) { cost = c; pair = two; own_per = per; }
+    }
+  const int prefix_ctas = prefix_tiles << pair, own_ctas = (own_tiles + own_per - 1) / own_per;
+  cfg.gridDim = dim3((unsigned)((prefix_ctas + a.n * own_ctas + pair) >> pair << pair), (unsigned)a.Hkv);
   cfg.blockDim = dim3(SW_THREADS); cfg.dynamicSmemBytes = SwCfg<HD>::SMEM;
-  return cudaLaunchKernelEx(&cfg, scored_weights_kernel<HD>, a, rb, prefix_tiles, own_ctas, own_per, 1.4426950408889634f / sqrtf((float)HD), mq, mpk, mok);
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.numAttrs = 1 + pair;
+  return cudaLaunchKernelEx(&cfg, scored_weights_kernel<HD>, a, rb, prefix_ctas, pair, own_ctas, own_per, 1.4426950408889634f / sqrtf((float)HD), mq, mpk, mok);
 }
 
 cudaError_t init_scored() {
@@ -765,13 +806,42 @@ static int sc_chunk(const ScoredArgs& a, int sm_count) {
   return (int)chunk;
 }
 
+// Many rows: prefix and own segments in chunks of at most `m` tiles of 128 keys, m by a CTA's time (about 2 us a tile and two and a
+// half tiles' worth of fixed cost) and the waves that all CTAs make, two an SM.  (The plan of mlora_attention cuts the prefix first and
+// the own segments then: at 8 x 32 nodes, 2048 + 1056 keys, it leaves own segments whole and takes 28 us, this 19.)
+static long long sw_ctas(const ScoredArgs& a, int m) {
+  const int G = a.Hq / a.Hkv, rb = G * (SW_ROWS / G);
+  const long long blocks = ((long long)a.n * a.T * G + rb - 1) / rb, rb_own = (a.T * G + rb - 1) / rb;
+  const long long tiles = (a.P + SW_KEYS - 1) / SW_KEYS, own = (a.suffix_bound + a.T + SW_KEYS - 1) / SW_KEYS;
+  return a.Hkv * ((tiles + m - 1) / m * blocks + (own + m - 1) / m * a.n * rb_own);
+}
+static void sw_chunks(ScoredArgs& a, int sm_count) {
+  const int tiles = (a.P + SW_KEYS - 1) / SW_KEYS, own = (a.suffix_bound + a.T + SW_KEYS - 1) / SW_KEYS, most = tiles > own ? tiles : own;
+  int best = most;
+  double cost = 0.0;
+  for (int m = most; m >= 1; m -= 1 + m / 16) {
+    const long long ctas = sw_ctas(a, m);
+    if (m < most && ctas > 4ll * sm_count) break;
+    const double c = (double)((ctas + 2 * sm_count - 1) / (2 * sm_count)) * (2.5 + m);
+    if (m == most || c < cost) { cost = c; best = m; }
+  }
+  a.attn.n_prefix_chunks = (tiles + best - 1) / best;
+  a.attn.prefix_chunk = (tiles > 0 ? (tiles + a.attn.n_prefix_chunks - 1) / a.attn.n_prefix_chunks : 1) * SW_KEYS;
+  a.attn.n_own_chunks = (own + best - 1) / best;
+  a.attn.own_chunk = (own + a.attn.n_own_chunks - 1) / a.attn.n_own_chunks * SW_KEYS;
+  // (evened out, the last chunks may be empty)
+  if (tiles > 0) a.attn.n_prefix_chunks = (tiles * SW_KEYS + a.attn.prefix_chunk - 1) / a.attn.prefix_chunk;
+  a.attn.n_own_chunks = (own * SW_KEYS + a.attn.own_chunk - 1) / a.attn.own_chunk;
+}
+
 void scored_plan(ScoredArgs& a, int sm_count) {
   const int G = a.Hq / a.Hkv;
   a.tc = sc_tc(a);
   if (a.tc) {
     a.attn = AttnArgs{};
     a.attn.P = a.P; a.attn.n = a.n; a.attn.T = a.T; a.attn.Hq = a.Hq; a.attn.Hkv = a.Hkv; a.attn.hd = a.hd; a.attn.suffix_bound = a.suffix_bound;
-    attn_plan_tc(a.attn, sm_count);
+    a.attn.tc_nq = 1;
+    sw_chunks(a, sm_count);
     return;
   }
   const long long own_keys = (long long)a.suffix_bound + a.T;
@@ -799,10 +869,10 @@ size_t scored_workspace_most(const ScoredArgs& given, int sm_count) {
   ScoredArgs a = given;
   scored_plan(a, sm_count);
   if (a.tc) {
-    // an own segment is cut in at most so many chunks as two CTAs an SM take, or tiles
-    const int G = a.Hq / a.Hkv, rb = G * (SW_ROWS / G), per_chunk = a.Hkv * a.n * ((a.T * G + rb - 1) / rb);
-    const int tiles = (a.suffix_bound + a.T + SW_KEYS - 1) / SW_KEYS, most = 2 * sm_count / per_chunk;
-    return sw_floats(a, (size_t)a.attn.n_prefix_chunks + (tiles < most ? tiles : (most > 1 ? most : 1)));
+    // a CTA writes at most 128 rows of partial results; there are no more than four an SM, or one for each item, or one a tile
+    const long long items = sw_ctas(a, 1 << 28), all = sw_ctas(a, 1), four = 4ll * sm_count;
+    const long long ctas = all < four ? all : (items > four ? items : four);
+    return sw_floats(a, 0) + (size_t)(SW_ROWS * ctas) * (a.hd + 2);
   }
   // a CTA writes 16 rows of partial results; there are never more than four waves of CTAs and one for each item, nor more than
   // rounds of keys and one for each item (sc_chunk)
