@@ -11,6 +11,8 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <type_traits>
+
 #include "../../include/mlora.h"
 #include "cache_ops.cuh"
 #include "tc.cuh"
@@ -259,9 +261,9 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
   }
 }
 
-constexpr int FIN_THREADS = 128, FIN_KEYS = 128;
+constexpr int FIN_THREADS = 128, FIN_WARPS = FIN_THREADS / 32, FIN_KEYS = 128;   // keys of a warp, four a lane
 constexpr int FIN_ROWS = 512;                              // rows whose maximum and 1 / sum are held at a time
-constexpr int FIN_FLY = 8;                                 // reads of a thread on their way at a time
+constexpr int FIN_FLY = 8, FIN_ONE = 16;                   // 16-byte, 4-byte reads of a thread on their way at a time
 
 __device__ __forceinline__ int sc_len(const ScoredArgs& p, int s) {
   const int S = p.suffix_len[s];
@@ -320,19 +322,20 @@ __device__ __forceinline__ float2 sc_join_row(const ScoredArgs& p, int w, int R_
   return make_float2(M == -INFINITY ? 0.f : M, inv);
 }
 
-// Blocks: rows of the output (one warp a row), then the prefix keys (a lane has four keys; a warp all rows of up to eight, else every
-// fourth row of the block's 128 keys), then the own keys.  Bound by the length of its chain of reads, so everything whose address is known goes out first: partial results
+// Blocks: rows of the output (one warp a row), then the prefix keys, then the own keys.  Of up to eight rows a warp takes all, for 128
+// keys (four a lane); of more every fourth, for the block's 128 keys, or 32 (one a lane; ONE) where there would be few blocks.
+// Bound by the length of its chain of reads, so everything whose address is known goes out first: partial results
 // and scores before the length, maxima and sums that say what they count for (memory of the workspace in any case, never written
-// in vain).  A row's chunks are joined by several lanes at once.
-template <int HD>
-__global__ void __launch_bounds__(FIN_THREADS) scored_finish_kernel(const ScoredArgs p, const int out_blocks, const int prefix_blocks, const int own_blocks) {
+// in vain).
+template <int HD, bool ONE>
+__global__ void __launch_bounds__(FIN_THREADS, 5) scored_finish_kernel(const ScoredArgs p, const int out_blocks, const int prefix_blocks, const int own_blocks,
+                                                                    const int prefix_keys, const int own_keys) {
   __shared__ float2 row_s[FIN_ROWS];
-  __shared__ __align__(16) float sum_s[FIN_THREADS / 32][FIN_KEYS];
+  __shared__ __align__(16) float sum_s[FIN_WARPS][FIN_KEYS];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = p.Hq / p.Hkv, R = p.T * G, R_all = p.n * R, slots = p.n_prefix_chunks + p.n_own_chunks;
-  const float2* const ml_all = reinterpret_cast<const float2*>(p.part_ml);
   int b = blockIdx.x;
   if (b < out_blocks) {
-    const int w = b * (FIN_THREADS / 32) + warp;
+    const int w = b * FIN_WARPS + warp;
     if (w >= p.Hkv * R_all) return;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     sc_join_row<HD>(p, w, R_all, slots, lane, [&](int s) { return sc_slots(p, s); });
@@ -340,45 +343,60 @@ __global__ void __launch_bounds__(FIN_THREADS) scored_finish_kernel(const Scored
   }
   b -= out_blocks;
   const bool own = b >= p.Hkv * prefix_blocks;
-  int kh, s = 0, key0, step, v0, v1, ld, limit;            // the block's 128 keys from key0 on, then those `step` keys on, ...
+  int kh, s = 0, key0, v0, v1, ld, limit;
+  const int keys = own ? own_keys : prefix_keys;           // of the block: 512 (few rows), 128 or 32
+  const int step = (own ? own_blocks : prefix_blocks) * keys;          // the block's next keys are so many on
   const float* sc;
   float* dst;
   if (!own) {
-    kh = b / prefix_blocks; key0 = (b - kh * prefix_blocks) * FIN_KEYS; step = prefix_blocks * FIN_KEYS;
+    kh = b / prefix_blocks; key0 = (b - kh * prefix_blocks) * keys;
     v0 = 0; v1 = R_all; ld = p.ld_prefix; sc = p.sc_prefix; limit = p.P;
     dst = p.prefix_weight + (size_t)kh * p.P;
   } else {
     b -= p.Hkv * prefix_blocks;
     const int seg = b / own_blocks;
-    kh = seg % p.Hkv; s = seg / p.Hkv; key0 = (b - seg * own_blocks) * FIN_KEYS; step = own_blocks * FIN_KEYS;
+    kh = seg % p.Hkv; s = seg / p.Hkv; key0 = (b - seg * own_blocks) * keys;
     v0 = s * R; v1 = v0 + R; ld = p.ld_own; sc = p.sc_own;
     dst = p.own_weight + ((size_t)s * p.Hkv + kh) * p.cap;
     limit = sc_len(p, s) + p.T;
     if (key0 >= limit) return;
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  float4 x[FIN_FLY];
-  const int r_step = v1 - v0 <= FIN_FLY ? 1 : 4;
-  auto fetch = [&](int k0, int r0, int rows, int r) {      // keys k0 + 4 lane ... of rows r0 + r, r0 + r + r_step, ...
-    const float* const at = sc + ((size_t)kh * R_all + r0) * ld + min(k0 + 4 * lane, ld - 4);   // (a scratch row is a multiple of 16 keys)
+  const bool all_rows = keys > FIN_KEYS, one = ONE && keys < FIN_KEYS;
+  const int r_step = all_rows ? 1 : FIN_WARPS;
+  float x[4 * FIN_FLY];                                    // scores: four keys of FIN_FLY rows, or one key of FIN_ONE rows
+  auto fetch = [&](int k0, int r0, int rows, int r) {      // the lane's keys from k0 on, of rows r0 + r, r0 + r + r_step, ...
+    // (a scratch row is a multiple of 16 keys long; what lies past the last key is read and not used)
+    const float* const at = sc + ((size_t)kh * R_all + r0) * ld + (one ? min(k0 + lane, ld - 1) : min(k0 + 4 * lane, ld - 4));
+    if (one) {
 #pragma unroll
-    for (int i = 0; i < FIN_FLY; ++i)
-      if (r + i * r_step < rows)
-        asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[i].x), "=f"(x[i].y), "=f"(x[i].z), "=f"(x[i].w) : "l"(at + (size_t)(r + i * r_step) * ld) : "memory");
+      for (int i = 0; i < FIN_ONE; ++i)
+        if (r + i * FIN_WARPS < rows) asm volatile("ld.global.cg.f32 %0, [%1];" : "=f"(x[i]) : "l"(at + (size_t)(r + i * FIN_WARPS) * ld) : "memory");
+    } else {
+#pragma unroll
+      for (int i = 0; i < FIN_FLY; ++i)
+        if (r + i * r_step < rows)
+          asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[4 * i]), "=f"(x[4 * i + 1]), "=f"(x[4 * i + 2]), "=f"(x[4 * i + 3])
+                       : "l"(at + (size_t)(r + i * r_step) * ld) : "memory");
+    }
   };
-  auto normalisers = [&](int r0, int rows) {               // eight lanes a row
-    for (int r = tid >> 3; r < ((rows + 15) & ~15); r += FIN_THREADS / 8) {
-      const int v = r0 + min(r, rows - 1), ns = sc_slots(p, v / R), l = lane & 7;
-      const float2* const ml_at = ml_all + ((size_t)kh * R_all + v) * slots;
+  // Eight lanes a row where there are few rows, else one.
+  auto normalise = [&](auto lanes_c, int r0, int rows) {
+    constexpr int lanes = decltype(lanes_c)::value, per = FIN_THREADS / lanes;
+    const int l = tid & (lanes - 1);
+    for (int r = tid / lanes; r < (rows + per - 1) / per * per; r += per) {
+      const int v = r0 + min(r, rows - 1), ns = sc_slots(p, v / R);
+      const float2* const ml_at = reinterpret_cast<const float2*>(p.part_ml) + ((size_t)kh * R_all + v) * slots;
       float M = -INFINITY, L = 0.f;
-      for (int i = l; i < ns; i += 8) {
+#pragma unroll 4
+      for (int i = l; i < ns; i += lanes) {
         const float2 ml = __ldcg(ml_at + i);
         const float Mn = fmaxf(M, ml.x), Mb = Mn == -INFINITY ? 0.f : Mn;
         L = L * sc_ex2(M - Mb) + ml.y * sc_ex2(ml.x - Mb);
         M = Mn;
       }
 #pragma unroll
-      for (int o = 1; o < 8; o <<= 1) {
+      for (int o = 1; o < lanes; o <<= 1) {
         const float Mo = __shfl_xor_sync(0xffffffffu, M, o), Lo = __shfl_xor_sync(0xffffffffu, L, o);
         const float Mn = fmaxf(M, Mo), Mb = Mn == -INFINITY ? 0.f : Mn;
         L = L * sc_ex2(M - Mb) + Lo * sc_ex2(Mo - Mb);
@@ -387,17 +405,19 @@ __global__ void __launch_bounds__(FIN_THREADS) scored_finish_kernel(const Scored
       if (l == 0 && r < rows) row_s[r] = make_float2(M == -INFINITY ? 0.f : M, 1.f / L);
     }
   };
-  if (v1 - v0 <= FIN_FLY) {
-    // few rows: every warp takes 128 keys of its own, all rows at once
+  auto normalisers = [&](int r0, int rows) {
+    if (rows <= 2 * FIN_THREADS / 8) normalise(std::integral_constant<int, 8>{}, r0, rows);
+    else normalise(std::integral_constant<int, 1>{}, r0, rows);
+  };
+  if (all_rows) {
     const int rows = v1 - v0;
-    key0 += (key0 / FIN_KEYS * 3 + warp) * FIN_KEYS;       // (block i: keys 512 i ...)
-    step *= 4;
-    fetch(key0, v0, rows, 0);
-    normalisers(v0, rows);
+    const int mine = key0 + warp * FIN_KEYS;
+    fetch(mine, v0, rows, 0);
+    normalise(std::integral_constant<int, 8>{}, v0, rows);
     __syncthreads();
-    for (int k0 = key0; k0 < limit; k0 += step) {
+    for (int k0 = mine; k0 < limit; k0 += step) {
       const int k = k0 + 4 * lane;
-      if (k0 != key0) fetch(k0, v0, rows, 0);
+      if (k0 != mine) fetch(k0, v0, rows, 0);
       float old[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 4; ++i) old[i] = k + i < limit ? dst[k + i] : 0.f;
@@ -405,8 +425,8 @@ __global__ void __launch_bounds__(FIN_THREADS) scored_finish_kernel(const Scored
       for (int i = 0; i < FIN_FLY; ++i)
         if (i < rows) {
           const float2 ml = row_s[i];
-          sum[0] = fmaf(sc_ex2(x[i].x - ml.x), ml.y, sum[0]); sum[1] = fmaf(sc_ex2(x[i].y - ml.x), ml.y, sum[1]);
-          sum[2] = fmaf(sc_ex2(x[i].z - ml.x), ml.y, sum[2]); sum[3] = fmaf(sc_ex2(x[i].w - ml.x), ml.y, sum[3]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sum[j] = fmaf(sc_ex2(x[4 * i + j] - ml.x), ml.y, sum[j]);
         }
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -416,7 +436,8 @@ __global__ void __launch_bounds__(FIN_THREADS) scored_finish_kernel(const Scored
   }
   const bool once = v1 - v0 <= FIN_ROWS;                   // the rows' normalisers are made once
   for (int k0 = key0; k0 < limit; k0 += step) {
-    const float old = k0 + tid < limit ? dst[k0 + tid] : 0.f;
+    const bool writes = tid < keys && k0 + tid < limit;
+    const float old = writes ? dst[k0 + tid] : 0.f;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     for (int r0 = v0; r0 < v1; r0 += FIN_ROWS) {
       const int rows = min(FIN_ROWS, v1 - r0);
@@ -426,21 +447,36 @@ __global__ void __launch_bounds__(FIN_THREADS) scored_finish_kernel(const Scored
         normalisers(r0, rows);
         __syncthreads();
       }
-      for (int r = warp; r < rows; r += 4 * FIN_FLY) {
-        if (r != warp) fetch(k0, r0, rows, r);
+      if (one) {
+        for (int r = warp; r < rows; r += FIN_WARPS * FIN_ONE) {
+          if (r != warp) fetch(k0, r0, rows, r);
 #pragma unroll
-        for (int i = 0; i < FIN_FLY; ++i)
-          if (r + i * 4 < rows) {
-            const float2 ml = row_s[r + i * 4];
-            sum[0] = fmaf(sc_ex2(x[i].x - ml.x), ml.y, sum[0]); sum[1] = fmaf(sc_ex2(x[i].y - ml.x), ml.y, sum[1]);
-            sum[2] = fmaf(sc_ex2(x[i].z - ml.x), ml.y, sum[2]); sum[3] = fmaf(sc_ex2(x[i].w - ml.x), ml.y, sum[3]);
-          }
+          for (int i = 0; i < FIN_ONE; ++i)
+            if (r + i * FIN_WARPS < rows) { const float2 ml = row_s[r + i * FIN_WARPS]; sum[i & 3] = fmaf(sc_ex2(x[i] - ml.x), ml.y, sum[i & 3]); }
+        }
+      } else {
+        for (int r = warp; r < rows; r += FIN_WARPS * FIN_FLY) {
+          if (r != warp) fetch(k0, r0, rows, r);
+#pragma unroll
+          for (int i = 0; i < FIN_FLY; ++i)
+            if (r + i * FIN_WARPS < rows) {
+              const float2 ml = row_s[r + i * FIN_WARPS];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) sum[j] = fmaf(sc_ex2(x[4 * i + j] - ml.x), ml.y, sum[j]);
+            }
+        }
       }
     }
     if (k0 != key0) __syncthreads();
-    *reinterpret_cast<float4*>(&sum_s[warp][4 * lane]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    if (one) sum_s[warp][lane] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    else *reinterpret_cast<float4*>(&sum_s[warp][4 * lane]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
     __syncthreads();
-    if (k0 + tid < limit) dst[k0 + tid] = old + ((sum_s[0][tid] + sum_s[1][tid]) + (sum_s[2][tid] + sum_s[3][tid]));
+    if (writes) {
+      float t = 0.f;
+#pragma unroll
+      for (int w = 0; w < FIN_WARPS; ++w) t += sum_s[w][tid];
+      dst[k0 + tid] = old + t;
+    }
   }
 }
 
@@ -461,10 +497,11 @@ template <int HD> struct SwCfg {
   static constexpr size_t SMEM = 3 * (size_t)TILE + 1024;
 };
 
+constexpr int JOIN_THREADS = 128;
 template <int HD>
-__global__ void __launch_bounds__(FIN_THREADS) scored_join_kernel(const ScoredArgs p) {
+__global__ void __launch_bounds__(JOIN_THREADS) scored_join_kernel(const ScoredArgs p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // (scored_weights_kernel, which waits for this one)
-  const int w = blockIdx.x * (FIN_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31, R_all = p.n * p.T * (p.Hq / p.Hkv);
+  const int w = blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31, R_all = p.n * p.T * (p.Hq / p.Hkv);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (w >= p.Hkv * R_all) return;
   const AttnArgs& t = p.attn;
@@ -732,7 +769,7 @@ static cudaError_t sw_launch(const ScoredArgs& a, cudaStream_t st) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = st;
-  cfg.gridDim = dim3((unsigned)((rows * a.Hq + FIN_THREADS / 32 - 1) / (FIN_THREADS / 32))); cfg.blockDim = dim3(FIN_THREADS);
+  cfg.gridDim = dim3((unsigned)((rows * a.Hq + JOIN_THREADS / 32 - 1) / (JOIN_THREADS / 32))); cfg.blockDim = dim3(JOIN_THREADS);
   if ((e = cudaLaunchKernelEx(&cfg, scored_join_kernel<HD>, a)) != cudaSuccess) return e;
   const cuuint64_t H = sizeof(__half);
   CUtensorMap mq, mpk, mok;
@@ -779,7 +816,8 @@ cudaError_t init_scored() {
   cudaError_t e;
   if ((e = full_carveout(scored_weights_kernel<64>)) != cudaSuccess || (e = full_carveout(scored_weights_kernel<128>)) != cudaSuccess) return e;
   if ((e = full_carveout(scored_rows_kernel<64>)) != cudaSuccess || (e = full_carveout(scored_rows_kernel<128>)) != cudaSuccess) return e;
-  if ((e = full_carveout(scored_finish_kernel<64>)) != cudaSuccess || (e = full_carveout(scored_finish_kernel<128>)) != cudaSuccess) return e;
+  if ((e = full_carveout(scored_finish_kernel<64, false>)) != cudaSuccess || (e = full_carveout(scored_finish_kernel<128, false>)) != cudaSuccess ||
+      (e = full_carveout(scored_finish_kernel<64, true>)) != cudaSuccess || (e = full_carveout(scored_finish_kernel<128, true>)) != cudaSuccess) return e;
   if ((e = cudaFuncSetAttribute(scored_rows_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ScCfg<64>::SMEM)) != cudaSuccess) return e;
   if ((e = cudaFuncSetAttribute(scored_rows_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ScCfg<128>::SMEM)) != cudaSuccess) return e;
   if ((e = cudaFuncSetAttribute(scored_weights_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SwCfg<64>::SMEM)) != cudaSuccess) return e;
@@ -787,12 +825,23 @@ cudaError_t init_scored() {
 }
 
 // ----------------------------------------------------------------------------- plan
-// The tcgen05 kernels from more than 16 rows a stream and KV head on.
-static bool sc_tc(const ScoredArgs& a) { const int G = a.Hq / a.Hkv; return a.T * G > 16 && G <= SW_ROWS && tensor_maps_available(); }
+// The tcgen05 kernels where a stream has more than 16 rows a KV head and the scores in scratch would be many: from 3 million words on (heads
+// of 64 features; 2.25 of 128), or more than 256 rows that share the prefix.  16 x 32 heads of 64, prefix 512, 64 own keys, one stream
+// (0.3 M words): 9.0 us by the kernels for few rows, 12.9 by these; 8 x 8 x 32 rows, 512 + 1000 keys (3.1 M) 18.0 and 20.5, 2048 + 200 keys
+// (4.6 M) 26.4 and 20.6; 8 x 16 x 32 rows, 512 + 64 keys 27.6 and 17.8; 16 x 6 x 32, no prefix, 100 keys 11.1 and 14.6.
+static int sc_resident(const ScoredArgs& a, int sm_count) { return sm_count * (a.hd == 64 ? ScCfg<64>::CTAS : ScCfg<128>::CTAS); }
+static size_t sc_rows(const ScoredArgs& a) { return (size_t)a.n * a.T * a.Hq; }
+static bool sc_tc_shape(const ScoredArgs& a) { const int G = a.Hq / a.Hkv; return a.T * G > 16 && G <= SW_ROWS && tensor_maps_available(); }
+// the longest own segments that the kernels for few rows take where the others could (negative: none)
+static long long sc_few_bound(const ScoredArgs& a, int sm_count) {
+  const int G = a.Hq / a.Hkv;
+  if ((a.P > 0 && (long long)a.n * a.T * G > 256) || (long long)a.Hkv * a.n * ((a.T * G + 15) / 16) > sc_resident(a, sm_count)) return -1;
+  return (a.hd == 64 ? 3000000ll : 2250000ll) / (long long)sc_rows(a) - a.P - a.T;
+}
+static bool sc_tc(const ScoredArgs& a, int sm_count) { return sc_tc_shape(a) && a.suffix_bound > sc_few_bound(a, sm_count); }
 
 // Few rows: the keys in chunks that make one wave of CTAs where that is possible (chunks of at least a round of keys), else
 // four waves.  `work` = keys times 16-row tiles of all KV heads.
-static int sc_resident(const ScoredArgs& a, int sm_count) { return sm_count * (a.hd == 64 ? ScCfg<64>::CTAS : ScCfg<128>::CTAS); }
 static long long sc_work(const ScoredArgs& a) {
   return a.Hkv * (a.rt_prefix * (long long)a.P + (long long)a.n * a.rt_own * ((long long)a.suffix_bound + a.T));
 }
@@ -834,17 +883,10 @@ static void sw_chunks(ScoredArgs& a, int sm_count) {
   a.attn.n_own_chunks = (own * SW_KEYS + a.attn.own_chunk - 1) / a.attn.own_chunk;
 }
 
-void scored_plan(ScoredArgs& a, int sm_count) {
+static void sc_plan_few(ScoredArgs& a, int sm_count) {
   const int G = a.Hq / a.Hkv;
-  a.tc = sc_tc(a);
-  if (a.tc) {
-    a.attn = AttnArgs{};
-    a.attn.P = a.P; a.attn.n = a.n; a.attn.T = a.T; a.attn.Hq = a.Hq; a.attn.Hkv = a.Hkv; a.attn.hd = a.hd; a.attn.suffix_bound = a.suffix_bound;
-    a.attn.tc_nq = 1;
-    sw_chunks(a, sm_count);
-    return;
-  }
   const long long own_keys = (long long)a.suffix_bound + a.T;
+  a.tc = 0;
   a.rt_own = (a.T * G + 15) / 16;
   a.rt_prefix = (a.n * a.T * G + 15) / 16;
   const int chunk = sc_chunk(a, sm_count);
@@ -855,7 +897,15 @@ void scored_plan(ScoredArgs& a, int sm_count) {
   a.ld_own = (int)((own_keys + 15) / 16 * 16);
 }
 
-static size_t sc_rows(const ScoredArgs& a) { return (size_t)a.n * a.T * a.Hq; }
+void scored_plan(ScoredArgs& a, int sm_count) {
+  if (!sc_tc(a, sm_count)) { sc_plan_few(a, sm_count); return; }
+  a.tc = 1;
+  a.attn = AttnArgs{};
+  a.attn.P = a.P; a.attn.n = a.n; a.attn.T = a.T; a.attn.Hq = a.Hq; a.attn.Hkv = a.Hkv; a.attn.hd = a.hd; a.attn.suffix_bound = a.suffix_bound;
+  a.attn.tc_nq = 1;
+  sw_chunks(a, sm_count);
+}
+
 // tcgen05 form, behind the partial results: the rows' normalisers, masks (two floats a node), depths and lengths
 static size_t sw_floats(const ScoredArgs& a, size_t slots) { return sc_rows(a) * slots * (a.hd + 2) + sc_rows(a) * 2 + ((size_t)a.n * a.T + 1) * 4 + a.n; }
 static size_t sc_floats(const ScoredArgs& a) {
@@ -865,20 +915,27 @@ size_t scored_workspace_floats(const ScoredArgs& a) {
   return a.tc ? sw_floats(a, (size_t)a.attn.n_prefix_chunks + a.attn.n_own_chunks) : sc_floats(a);
 }
 
+// Each form needs more for a longer bound.
 size_t scored_workspace_most(const ScoredArgs& given, int sm_count) {
   ScoredArgs a = given;
-  scored_plan(a, sm_count);
-  if (a.tc) {
+  size_t most = 0;
+  long long few = a.suffix_bound;                          // the longest bound up to this one that goes by the kernels for few rows
+  if (sc_tc(a, sm_count)) {
     // a CTA writes at most 128 rows of partial results; there are no more than four an SM, or one for each item, or one a tile
     const long long items = sw_ctas(a, 1 << 28), all = sw_ctas(a, 1), four = 4ll * sm_count;
     const long long ctas = all < four ? all : (items > four ? items : four);
-    return sw_floats(a, 0) + (size_t)(SW_ROWS * ctas) * (a.hd + 2);
+    most = sw_floats(a, 0) + (size_t)(SW_ROWS * ctas) * (a.hd + 2);
+    few = sc_few_bound(a, sm_count);
+    if (few < 0) return most;
   }
+  a.suffix_bound = (int)few;
+  sc_plan_few(a, sm_count);
   // a CTA writes 16 rows of partial results; there are never more than four waves of CTAs and one for each item, nor more than
   // rounds of keys and one for each item (sc_chunk)
   const long long items = (long long)a.Hkv * ((long long)a.n * a.rt_own + a.rt_prefix);
   const long long waves = 4ll * sc_resident(a, sm_count), rounds = sc_work(a) / SC_KEYS + 1;
-  return (size_t)(16 * ((waves < rounds ? waves : rounds) + items)) * (a.hd + 2) + sc_rows(a) * ((size_t)a.ld_prefix + a.ld_own);
+  const size_t f = (size_t)(16 * ((waves < rounds ? waves : rounds) + items)) * (a.hd + 2) + sc_rows(a) * ((size_t)a.ld_prefix + a.ld_own);
+  return f > most ? f : most;
 }
 
 void scored_carve(ScoredArgs& a, float* ws) {              // ws: 16-byte aligned
@@ -905,22 +962,27 @@ static cudaError_t sc_launch(const ScoredArgs& a, cudaStream_t st) {
   scored_rows_kernel<HD><<<dim3((unsigned)(a.n_prefix_chunks * a.rt_prefix + a.n * a.n_own_chunks * a.rt_own), (unsigned)a.Hkv), SC_WARPS * 32, ScCfg<HD>::SMEM, st>>>(a, scale_log2);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const int out_blocks = (a.n * a.T * a.Hq + FIN_THREADS / 32 - 1) / (FIN_THREADS / 32);
-  // (long segments: a block for every 128 keys only as far as that fills the machine, the rest in turns)
-  auto blocks_of = [](long long keys, long long segments, int rows) {
-    const int per = rows <= FIN_FLY ? 4 * FIN_KEYS : FIN_KEYS;
+  const int out_blocks = (a.n * a.T * a.Hq + FIN_WARPS - 1) / FIN_WARPS;
+  // keys of a block, and blocks: one for all keys only as far as that fills the machine, the rest in turns
+  auto keys_of = [](long long keys, long long segments, int rows) {
+    return rows <= FIN_FLY ? FIN_WARPS * FIN_KEYS : (segments * ((keys + FIN_KEYS - 1) / FIN_KEYS) < 2 * 148 ? 32 : FIN_KEYS);
+  };
+  auto blocks_of = [](long long keys, long long segments, int per) {
     const long long all = (keys + per - 1) / per, fill = (148 * 16 + segments - 1) / segments;
     return (int)(all < fill ? all : fill);
   };
-  const int prefix_blocks = a.prefix_weight != nullptr ? blocks_of(a.P, a.Hkv, a.n * a.T * (a.Hq / a.Hkv)) : 0;
-  const int own_blocks = blocks_of((long long)a.suffix_bound + a.T, (long long)a.n * a.Hkv, a.T * (a.Hq / a.Hkv));
+  const int G = a.Hq / a.Hkv, own_all = a.suffix_bound + a.T;
+  const int prefix_keys = keys_of(a.P, a.Hkv, a.n * a.T * G), own_keys = keys_of(own_all, (long long)a.n * a.Hkv, a.T * G);
+  const int prefix_blocks = a.prefix_weight != nullptr ? blocks_of(a.P, a.Hkv, prefix_keys) : 0;
+  const int own_blocks = blocks_of(own_all, (long long)a.n * a.Hkv, own_keys);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(out_blocks + a.Hkv * prefix_blocks + a.n * a.Hkv * own_blocks)); cfg.blockDim = dim3(FIN_THREADS); cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, scored_finish_kernel<HD>, a, out_blocks, prefix_blocks, own_blocks);
+  const bool one = prefix_keys < FIN_KEYS || own_keys < FIN_KEYS;
+  return cudaLaunchKernelEx(&cfg, one ? scored_finish_kernel<HD, true> : scored_finish_kernel<HD, false>, a, out_blocks, prefix_blocks, own_blocks, prefix_keys, own_keys);
 }
 
 cudaError_t launch_attention_scored(const ScoredArgs& a, cudaStream_t st) {

@@ -2027,7 +2027,7 @@ int mlora_rope_append(const void* q, const void* k, const void* v, int32_t in_fp
   if (!q && !app) return fail(MLORA_ERR_ARG, "rope_append: nothing to do");
   if (app && (!suffix_len || !status)) return fail(MLORA_ERR_ARG, "rope_append: null suffix_len or status");
   if (!app && (own_weight || own_position)) return fail(MLORA_ERR_ARG, "rope_append: own_weight and own_position belong to appended rows");
-  if (n <= 0 || T <= 0 || (q && Hq <= 0) || (app && Hkv <= 0) || (long long)n * T > (1 << 28) || Hq < 0 || Hkv < 0 || Hq + 2ll * Hkv > (1 << 16))
+  if (n <= 0 || T <= 0 || (q && Hq <= 0) || (app && Hkv <= 0) || (long long)n * T > (1 << 28) || Hq < 0 || Hkv < 0 || Hq + 2ll * Hkv > (1 << 13))
     return fail(MLORA_ERR_ARG, "rope_append: bad shape");
   if (hd != 64 && hd != 128) return fail(MLORA_ERR_UNSUPPORTED, "rope_append: head_dim must be 64 or 128");
   if (rotary_dim < 16 || rotary_dim > hd || rotary_dim % 16) return fail(MLORA_ERR_UNSUPPORTED, "rope_append: rotary_dim must be a multiple of 16 up to head_dim");
