@@ -506,7 +506,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) scored_join_kernel(const ScoredA
   if (w >= p.Hkv * R_all) return;
   const AttnArgs& t = p.attn;
   const float2 ml = sc_join_row<HD>(p, w, R_all, t.n_prefix_chunks + t.n_own_chunks, lane, [&](int s) {
-    return t.n_prefix_chunks + min(t.n_own_chunks, (p.lens[s] + p.T + t.own_chunk - 1) / t.own_chunk); });
+    return t.n_prefix_chunks + min(t.n_own_chunks, (sc_len(p, s) + p.T + t.own_chunk - 1) / t.own_chunk); });
   if (lane == 0) p.row_ml[w] = ml;
 }
 
@@ -537,12 +537,10 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
       if (second) { v_lo = mine * rb; units -= mine; } else { units = mine; v_hi = min(R_all, mine * rb); }
     }
   } else {
-    // (the lengths are written by this call)
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int i = blockIdx.x - prefix_ctas;
     if (i >= p.n * own_ctas) return;                       // (the grid is made of whole clusters)
     s = i / own_ctas; key0 = (i - s * own_ctas) * own_per * SW_KEYS;
-    S = p.lens[s]; limit = S + p.T;
+    S = sc_len(p, s); limit = S + p.T;
     v_lo = s * R; v_hi = v_lo + R;
     if (key0 >= limit) return;
     mov_k = R <= rb;                                       // (else own_per is 1)
@@ -622,7 +620,7 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
     __syncwarp();
   } else {
     // ---- weights: thread = key; a block's rows' normalisers are brought by the same threads, one row each, a unit ahead
-    if (!own) asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     float* const dst = own ? p.own_weight + ((size_t)s * p.Hkv + kh) * p.cap : p.prefix_weight + (size_t)kh * p.P;
     const bool tree = own && p.T > 1;
     bool alive = true;
@@ -725,14 +723,14 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
   if (warp == 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
 }
 
-// What the tcgen05 kernels read of the pass: lengths within their bound, every node's ancestor-or-self mask (a malformed parent
-// counts as the root, and is reported).
+// What the tcgen05 kernels read of the pass: every node's ancestor-or-self mask (a malformed parent counts as the root).  Reports that and
+// lengths out of their bound.
 __global__ void scored_prep_kernel(const ScoredArgs p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // (the attention kernel, which waits for this one)
   const int i = blockIdx.x * blockDim.x + threadIdx.x;
   if (i < p.n) {
     const int S = p.suffix_len[i];
     if (S < 0 || S > p.suffix_bound) atomicCAS(p.status, 0, MLORA_ERR_ARG);
-    p.lens[i] = S < 0 ? 0 : (S > p.suffix_bound ? p.suffix_bound : S);
   }
   if (i >= p.n * p.T) return;
   const int s = i / p.T;
@@ -762,7 +760,8 @@ static cudaError_t sw_launch(const ScoredArgs& a, cudaStream_t st) {
   AttnArgs t = a.attn;
   t.q = a.q; t.prefix_k = a.prefix_k; t.prefix_v = a.prefix_v; t.prefix_head_stride = (size_t)a.P * HD;
   t.own_k = a.own_k; t.own_v = a.own_v; t.own_head_stride = (size_t)a.cap * HD; t.own_stream_stride = t.own_head_stride * a.Hkv;
-  t.suffix_len = a.lens; t.anc = a.anc; t.depth = a.depth; t.out = a.out; t.status = a.status; t.part_o = a.part_o; t.part_ml = a.part_ml;
+  // (its CTAs start while the masks are made; the lengths are the caller's own, for which its chunks and copies stay in bounds whatever they say)
+  t.pdl = 1; t.anc_late = 1; t.suffix_len = a.suffix_len; t.anc = a.anc; t.depth = a.depth; t.out = a.out; t.status = a.status; t.part_o = a.part_o; t.part_ml = a.part_ml;
   if ((e = launch_attention(t, st)) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2];
@@ -906,8 +905,8 @@ void scored_plan(ScoredArgs& a, int sm_count) {
   sw_chunks(a, sm_count);
 }
 
-// tcgen05 form, behind the partial results: the rows' normalisers, masks (two floats a node), depths and lengths
-static size_t sw_floats(const ScoredArgs& a, size_t slots) { return sc_rows(a) * slots * (a.hd + 2) + sc_rows(a) * 2 + ((size_t)a.n * a.T + 1) * 4 + a.n; }
+// tcgen05 form, behind the partial results: the rows' normalisers, masks (two floats a node) and depths
+static size_t sw_floats(const ScoredArgs& a, size_t slots) { return sc_rows(a) * slots * (a.hd + 2) + sc_rows(a) * 2 + ((size_t)a.n * a.T + 1) * 4; }
 static size_t sc_floats(const ScoredArgs& a) {
   return sc_rows(a) * ((size_t)(a.n_prefix_chunks + a.n_own_chunks) * (a.hd + 2) + (size_t)a.ld_prefix + a.ld_own);
 }
@@ -947,7 +946,6 @@ void scored_carve(ScoredArgs& a, float* ws) {              // ws: 16-byte aligne
     a.row_ml = (float2*)at;
     a.anc = (unsigned long long*)(a.row_ml + sc_rows(a));
     a.depth = (int32_t*)(a.anc + (size_t)a.n * a.T);
-    a.lens = a.depth + (size_t)a.n * a.T;
     return;
   }
   const size_t parts = sc_rows(a) * ((size_t)a.n_prefix_chunks + a.n_own_chunks);

@@ -250,6 +250,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs p, const int rb_rows, const int 
     const uint32_t s_t = tmem + w * 128 + ((uint32_t)((warp & 3) * 32) << 16), o_t = s_t - w * 128 + NQ * 128 + w * HD;
     const int lim = !row_ok ? 0 : (p.causal ? p.P + m + 1 : it.k1);      // keys below it are visible (own segments: see the mask)
     unsigned long long anc = 0ull;
+    if (it.own && p.anc_late) asm volatile("griddepcontrol.wait;" ::: "memory");
     if (it.own && row_ok) anc = p.anc[m];
     float m_used = -INFINITY, l = 0.f;
     for (int j = 0; j < n_tiles; ++j) {

@@ -37,8 +37,8 @@ struct ScoredArgs {
   int tc;                               // many rows a KV head: the tcgen05 kernels
   AttnArgs attn;                        // ... their attention
   float2* row_ml;                       // ... scratch: the rows' (maximum, 1 / sum)
-  unsigned long long* anc;              // ... scratch: ancestor masks, clamped lengths, depths (not read)
-  int32_t *lens, *depth;
+  unsigned long long* anc;              // ... scratch: ancestor masks, depths (not read)
+  int32_t* depth;
 };
 cudaError_t init_scored();              // per device, once
 void scored_plan(ScoredArgs& a, int sm_count);

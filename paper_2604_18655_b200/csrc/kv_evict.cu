@@ -18,6 +18,7 @@
 namespace mlora {
 
 constexpr int EV_BINS = 2048;
+constexpr int EV_FEW = 4;                                  // up to so many rows too many are found one by one
 
 __device__ __forceinline__ uint32_t ev_image(float w) {
   if (w == 0.f) w = 0.f;
@@ -84,13 +85,16 @@ __device__ __forceinline__ int4 ev_remote4(const void* own, int rank) {
 
 // KPT: rows a thread holds in registers (0: any number, read again each time).  CL: the CTAs of a cluster share the segment.  Warp w of
 // CTA c has the rows from (c * WARPS + w) * 32 * KPT on (KPT = 0: an even share), lane l every 32nd of them.
-template <int THREADS, int KPT, bool CL>
+template <int THREADS, int KPT, bool CL, bool FEW>
 __global__ void __launch_bounds__(THREADS) kv_select_kernel(const EvictArgs p, const int move_here) {
   constexpr int WARPS = THREADS / 32, PER = EV_BINS / THREADS;
   __shared__ __align__(16) int hist[EV_BINS];
   __shared__ int s_w[2][WARPS];
   __shared__ uint32_t s_lo[WARPS], s_hi[WARPS];
   __shared__ int s_found[3], s_got[3];                     // bin, rows of the class above it, rows in it
+  __shared__ uint32_t s_few[2][3][WARPS];                  // few rows too many: a warp's last row (class, image, index)
+  __shared__ int s_gone[EV_FEW], s_few_moves;
+  __shared__ int2 s_few_list[EV_FEW];
   __shared__ int s_cta[2];
   __shared__ uint32_t s_range[2];
   int rank = 0, ctas = 1;
@@ -178,6 +182,92 @@ __global__ void __launch_bounds__(THREADS) kv_select_kernel(const EvictArgs p, c
     }
     return sum;
   };
+  const bool copy_w = p.out_weight != p.weight, copy_p = pos != nullptr && p.out_position != p.position, copies = copy_w || copy_p || p.out_source != nullptr;
+  auto copy = [&](uint32_t same) {                         // what stays where it is (all of a batch's reads ahead of its writes)
+#pragma unroll
+    for (int j0 = 0; j0 < CH; j0 += FLY) {
+      float x[FLY];
+      int32_t q[FLY];
+#pragma unroll
+      for (int j = 0; j < FLY; ++j) {
+        const int i = i0 + (j0 + j) * 32;
+        const bool ok = (same >> (j0 + j)) & 1u;
+        x[j] = ok && copy_w ? w[i] : 0.f;
+        q[j] = ok && copy_p ? pos[i] : 0;
+      }
+#pragma unroll
+      for (int j = 0; j < FLY; ++j) {
+        const int i = i0 + (j0 + j) * 32;
+        if (!((same >> (j0 + j)) & 1u)) continue;
+        if (copy_w) p.out_weight[base + i] = x[j];
+        if (copy_p) p.out_position[base + i] = q[j];
+        if (p.out_source != nullptr) p.out_source[(size_t)pair * B + i] = i;
+      }
+    }
+  };
+  // ---- a row or a few too many (a stream that decodes at its budget): the last of the order, one after the other -- the smallest image of
+  // the rows that are not new, or of the new ones where there are no others; of equals the highest index
+  if constexpr (FEW) {
+    const int drop = S - B;
+    uint32_t alive = there;
+    for (int d = 0; d < drop; ++d) {
+      uint32_t lowest = 0xffffffffu, lowest_new = 0xffffffffu;
+      bool any = false;
+#pragma unroll
+      for (int j = 0; j < CH; ++j)
+        if ((alive >> j) & 1u) {
+          if ((fresh >> j) & 1u) lowest_new = min(lowest_new, key[j]);
+          else { lowest = min(lowest, key[j]); any = true; }
+        }
+      lowest = __reduce_min_sync(0xffffffffu, lowest); lowest_new = __reduce_min_sync(0xffffffffu, lowest_new);
+      any = __any_sync(0xffffffffu, any);
+      // (images reach 0xff800000 at most: 0xffffffff stands for no row)
+      const uint32_t mine = any ? lowest : lowest_new;
+      int at = -1;
+#pragma unroll
+      for (int j = 0; j < CH; ++j)
+        if (((alive >> j) & 1u) && (bool)((fresh >> j) & 1u) != any && key[j] == mine) at = max(at, i0 + j * 32);
+      at = __reduce_max_sync(0xffffffffu, at);
+      if (lane == 0) { s_few[d & 1][0][warp] = any ? 0u : 1u; s_few[d & 1][1][warp] = mine; s_few[d & 1][2][warp] = (uint32_t)at; }
+      __syncthreads();
+      const uint32_t c = lane < WARPS ? s_few[d & 1][0][lane] : 1u, k = lane < WARPS ? s_few[d & 1][1][lane] : 0xffffffffu;
+      const int i = lane < WARPS ? (int)s_few[d & 1][2][lane] : -1;
+      const uint32_t c_min = __reduce_min_sync(0xffffffffu, c);        // (a warp without rows has class 1 and no image)
+      const uint32_t k_min = __reduce_min_sync(0xffffffffu, c == c_min ? k : 0xffffffffu);
+      const int gone = __reduce_max_sync(0xffffffffu, c == c_min && k == k_min ? i : -1);
+      if (tid == 0) s_gone[d] = gone;
+#pragma unroll
+      for (int j = 0; j < CH; ++j)
+        if (i0 + j * 32 == gone) alive &= ~(1u << j);
+    }
+    __syncthreads();
+    if (copies) copy(alive & up_to(B));
+    if (tid == 0) {                                        // the places before the budget, and the rows behind it that stay
+      int n_moves = 0, m = B;
+      for (int h = 0; h < drop; ++h) {                     // (in rising order: the smallest place not taken yet)
+        int place = B;
+        for (int d = 0; d < drop; ++d)
+          if (s_gone[d] < place && (n_moves == 0 || s_gone[d] > s_few_list[n_moves - 1].y)) place = s_gone[d];
+        if (place >= B) break;
+        bool gone = true;
+        while (m < S && gone) {
+          gone = false;
+          for (int d = 0; d < drop; ++d) gone = gone || s_gone[d] == m;
+          if (gone) ++m;
+        }
+        s_few_list[n_moves++] = make_int2(m++, place);
+      }
+      s_few_moves = n_moves;
+      p.counts[pair] = n_moves;
+      if (!move_here)
+        for (int i = 0; i < n_moves && i < p.max_moves; ++i) list[i] = s_few_list[i];
+    }
+    __syncthreads();
+    if (move_here) {
+      if (p.hd == 64) ev_move<64, 1>(p, s_few_list, s_few_moves, pair, tid / 16, THREADS / 16, tid % 16);
+      else ev_move<128, 1>(p, s_few_list, s_few_moves, pair, tid / 32, THREADS / 32, tid % 32);
+    }
+  } else {
   // ---- the class in which the order is decided: the new rows where they alone fill the budget, else the others
   bool among_new = false;
   int want = B;
@@ -327,7 +417,6 @@ __global__ void __launch_bounds__(THREADS) kv_select_kernel(const EvictArgs p, c
   int h_at = before(holes, n_h), m_at = before(movers, n_m);
   const int n_moves = min(min(n_h, n_m), p.max_moves);     // (the three agree: see above)
   if (tid == 0 && rank == 0) p.counts[pair] = n_moves;
-  const bool copy_w = p.out_weight != p.weight, copy_p = pos != nullptr && p.out_position != p.position, copies = copy_w || copy_p || p.out_source != nullptr;
   seen = seen0;
   pass([&] {
     if (KPT == 0) stay = stay_bits();
@@ -342,34 +431,14 @@ __global__ void __launch_bounds__(THREADS) kv_select_kernel(const EvictArgs p, c
         h_at += __popc(hm); m_at += __popc(mm);
       }
     }
-    if (copies) {                                          // what stays where it is (all of a batch's reads ahead of its writes)
-#pragma unroll
-      for (int j0 = 0; j0 < CH; j0 += FLY) {
-        float x[FLY];
-        int32_t q[FLY];
-#pragma unroll
-        for (int j = 0; j < FLY; ++j) {
-          const int i = i0 + (j0 + j) * 32;
-          const bool ok = (same >> (j0 + j)) & 1u;
-          x[j] = ok && copy_w ? w[i] : 0.f;
-          q[j] = ok && copy_p ? pos[i] : 0;
-        }
-#pragma unroll
-        for (int j = 0; j < FLY; ++j) {
-          const int i = i0 + (j0 + j) * 32;
-          if (!((same >> (j0 + j)) & 1u)) continue;
-          if (copy_w) p.out_weight[base + i] = x[j];
-          if (copy_p) p.out_position[base + i] = q[j];
-          if (p.out_source != nullptr) p.out_source[(size_t)pair * B + i] = i;
-        }
-      }
-    }
+    if (copies) copy(same);
   });
   // the list, through global memory; and no CTA of a cluster ends while another may read its counts
   if constexpr (CL) ev_cluster_sync(); else __syncthreads();
   if (move_here) {
     if (p.hd == 64) ev_move<64, 4>(p, list, n_moves, pair, rank * (THREADS / 16) + tid / 16, ctas * (THREADS / 16), tid % 16);
     else ev_move<128, 4>(p, list, n_moves, pair, rank * (THREADS / 32) + tid / 32, ctas * (THREADS / 32), tid % 32);
+  }
   }
 }
 
@@ -381,7 +450,7 @@ __global__ void __launch_bounds__(256) kv_move_kernel(const EvictArgs p) {
   ev_move<HD, 4>(p, p.moves + (size_t)pair * p.max_moves, p.counts[pair], pair, blockIdx.x * PER + threadIdx.x / LANES, gridDim.x * PER, threadIdx.x % LANES);
 }
 
-template <int THREADS, int KPT, bool CL>
+template <int THREADS, int KPT, bool CL, bool FEW = false>
 static cudaError_t ev_select(const EvictArgs& a, int ctas, int move_here, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(a.Hkv * ctas), (unsigned)a.n); cfg.blockDim = dim3(THREADS); cfg.stream = st;
@@ -389,13 +458,18 @@ static cudaError_t ev_select(const EvictArgs& a, int ctas, int move_here, cudaSt
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr; cfg.numAttrs = CL ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kv_select_kernel<THREADS, KPT, CL>, a, move_here);
+  return cudaLaunchKernelEx(&cfg, kv_select_kernel<THREADS, KPT, CL, FEW>, a, move_here);
 }
 
 cudaError_t launch_kv_evict(const EvictArgs& a, cudaStream_t st) {
   const int move_here = a.max_moves <= 256;
+  const bool few = a.bound - a.budget <= EV_FEW;           // (one row of 257 in eight segments: 2.9 us, 4.3 by histograms)
   cudaError_t e;
-  if (a.bound <= 1024) e = ev_select<256, 4, false>(a, 1, move_here, st);
+  if (few && a.bound <= 1024) e = ev_select<256, 4, false, true>(a, 1, move_here, st);
+  else if (few && a.bound <= 4096) e = ev_select<1024, 4, false, true>(a, 1, move_here, st);
+  else if (few && a.bound <= 8192) e = ev_select<1024, 8, false, true>(a, 1, move_here, st);
+  else if (few && a.bound <= 16384) e = ev_select<1024, 16, false, true>(a, 1, move_here, st);
+  else if (a.bound <= 1024) e = ev_select<256, 4, false>(a, 1, move_here, st);
   else if (a.bound <= 4096) e = ev_select<1024, 4, false>(a, 1, move_here, st);
   else if (a.bound <= 8192) e = ev_select<1024, 8, false>(a, 1, move_here, st);
   else if (a.bound <= 16384) e = ev_select<1024, 16, false>(a, 1, move_here, st);

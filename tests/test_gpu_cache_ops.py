@@ -555,3 +555,37 @@ def test_offsets_beyond_32_bits(mb):
     ref = dev(evict_reference(wh, np.arange(cap, dtype=np.int32), S[1] + 1, B, 10, S[1]))
     assert ol.tolist() == [6, B] and int(st.item()) == 0
     assert torch.equal(src[1, 8].long(), ref) and torch.equal(k[1, 8, :B], kh[ref]) and torch.equal(v[1, 8, :B], vh[ref])
+
+
+@pytest.mark.parametrize("n,T,Hq,Hkv,hd,P,bound", [(2, 1, 8, 2, 64, 100, 3000), (2, 9, 32, 8, 64, 700, 1500), (3, 20, 6, 2, 128, 64, 700), (1, 64, 16, 1, 64, 0, 9000)])
+def test_scored_workspace_serves_every_smaller_bound(mb, n, T, Hq, Hkv, hd, P, bound):
+    """One workspace of the largest bound's size, filled with NaN; the call sizes its chunks (and picks its kernels) by each bound."""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    r16 = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=torch.float16)  # noqa: E731
+    cap = bound + T
+    q, k, v = r16(n * T, Hq, hd), r16(n, Hkv, cap, hd), r16(n, Hkv, cap, hd)
+    pk, pv = (r16(Hkv, P, hd), r16(Hkv, P, hd)) if P else (None, None)
+    need = mb.mlora_attention_scored_workspace_bytes(n, T, Hq, Hkv, hd, P, bound)
+    ws, st = torch.full((need,), 255, dtype=torch.uint8, device="cuda"), status()
+    lens = i32([7] * n)
+    first = None
+    for b in sorted({7, 8, 63, 64, 127, 128, bound // 7, bound // 3, bound // 2, 2 * bound // 3, bound - 1, bound} | set(range(100, bound, bound // 23))):
+        out, w = torch.empty_like(q), torch.zeros(n, Hkv, cap, device="cuda")
+        ws.fill_(255)
+        mb.mlora_attention_scored(q, pk, pv, k, v, lens, b, None, out, w, None, ws, st)
+        if first is None:
+            first = (out.float(), w)
+        # the same keys in other chunks: rounding of weights to fp16 and of the output, sums in another order
+        assert float((out.float() - first[0]).abs().max()) <= 4 * 2.0**-11 * float(first[0].abs().max()) + 2.0**-9
+        assert float((w - first[1]).abs().max()) <= 2.0**-17 * float(first[1].max())
+    assert int(st.item()) == 0
+
+
+def test_evict_few_rows_too_many_in_every_place(mb):
+    """One to four rows over the budget: found one by one, as decoding at the budget does it"""
+    for over in (1, 2, 3, 4, 5):
+        for seed in range(6):
+            evict_case(mb, 2, 3, 64, [40 + over, 38], 40, [0, 5, 40][seed % 3], seed=seed, weights=["random", "ties", "special"][seed // 2], in_place=seed % 2 == 0)
+    evict_case(mb, 1, 2, 128, [3], 1, 1, seed=3)
+    evict_case(mb, 1, 2, 64, [4], 1, 0, seed=4, weights="ties")
+    evict_case(mb, 2, 1, 64, [5002, 5001], 5000, 100, seed=5, weights="ties", bound=7000)
