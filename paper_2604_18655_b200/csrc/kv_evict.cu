@@ -462,7 +462,10 @@ static cudaError_t ev_select(const EvictArgs& a, int ctas, int move_here, cudaSt
 }
 
 cudaError_t launch_kv_evict(const EvictArgs& a, cudaStream_t st) {
-  const int move_here = a.max_moves <= 256;
+  // The selecting CTAs move the rows themselves where these are few, or where the segments fill the SMs (one CTA each) to 60% in every
+  // wave: 256 segments 4096 -> 2048 rows 38.9 us, 43.0 by a kernel of their own; 160 segments 30.9 and 28.7, 16 segments 16.4 and 11.6.
+  const int pairs = a.n * a.Hkv, waves = (pairs + 147) / 148;
+  const int move_here = a.max_moves <= 256 || pairs * 5 >= waves * 148 * 3;
   const bool few = a.bound - a.budget <= EV_FEW;           // (one row of 257 in eight segments: 2.9 us, 4.3 by histograms)
   cudaError_t e;
   if (few && a.bound <= 1024) e = ev_select<256, 4, false, true>(a, 1, move_here, st);
@@ -477,7 +480,7 @@ cudaError_t launch_kv_evict(const EvictArgs& a, cudaStream_t st) {
   else e = ev_select<1024, 0, true>(a, 8, move_here, st);
   if (e != cudaSuccess || move_here) return e;
   cudaLaunchConfig_t cfg{};
-  const int per = 4 * (256 / (a.hd / 4)), most = (a.max_moves + per - 1) / per, pairs = a.n * a.Hkv;
+  const int per = 4 * (256 / (a.hd / 4)), most = (a.max_moves + per - 1) / per;
   const int want = (2 * 148 * 8 + pairs - 1) / pairs;
   cfg.gridDim = dim3((unsigned)(most < want ? most : want), (unsigned)pairs);
   cfg.blockDim = dim3(256); cfg.stream = st;
