@@ -106,18 +106,34 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
   constexpr int LPR = HD / 8, RPI = 32 / LPR;              // lanes a row, rows an instruction
   const int c_row = lane / LPR, c_piece = lane % LPR;
   const int steps = (k1 - k0 - warp * SC_STEP + SC_KEYS - 1) / SC_KEYS;           // (may be negative: none)
-  auto copy = [&](int i) {                                 // step i of this warp
-    if (i < steps) {
-      const int key0 = k0 + (i * SC_WARPS + warp) * SC_STEP;
-      const uint32_t dst = ring + (i % C::STAGES) * C::STEP;
+  const size_t c_first = (size_t)(k0 + warp * SC_STEP + c_row) * HD + c_piece * 8;
+  const __half *c_k = kb + c_first, *c_v = vb + c_first;
+  uint32_t c_at[SC_STEP / RPI];                            // where the lane's rows go within a step's K
 #pragma unroll
-      for (int r = 0; r < SC_STEP; r += RPI) {
-        const int row = r + c_row, key = key0 + row, n = key < k1 ? 16 : 0;
-        const uint32_t at = dst + (c_piece >> 3) * (SC_STEP * 128) + row * 128 + (((c_piece & 7) ^ (row & 7)) << 4);
-        const size_t from = (size_t)(key < k1 ? key : k0) * HD + c_piece * 8;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(kb + from), "r"(n) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + SC_STEP * HD * 2), "l"(vb + from), "r"(n) : "memory");
+  for (int r = 0; r < SC_STEP; r += RPI) c_at[r / RPI] = (c_piece >> 3) * (SC_STEP * 128) + (r + c_row) * 128 + (((c_piece & 7) ^ ((r + c_row) & 7)) << 4);
+  uint32_t c_stage = 0;
+  auto copy = [&](int i) {                                 // step i of this warp (in turn)
+    if (i < steps) {
+      const int left = k1 - (k0 + (i * SC_WARPS + warp) * SC_STEP) - c_row;       // the lane's rows from there on
+      const uint32_t dst = ring + c_stage;
+      c_stage = c_stage + C::STEP == C::STAGES * C::STEP ? 0 : c_stage + C::STEP;
+      if (left + c_row >= SC_STEP) {
+#pragma unroll
+        for (int r = 0; r < SC_STEP; r += RPI) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c_at[r / RPI]), "l"(c_k + r * HD) : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c_at[r / RPI] + SC_STEP * HD * 2), "l"(c_v + r * HD) : "memory");
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < SC_STEP; r += RPI) {
+          const int n = r < left ? 16 : 0;                 // (nothing is read where the count is 0; the address stays in the segment)
+          const size_t back = r < left ? (size_t)r * HD : 0;
+          const __half *fk = left > 0 ? c_k + back : kb, *fv = left > 0 ? c_v + back : vb;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + c_at[r / RPI]), "l"(fk), "r"(n) : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + c_at[r / RPI] + SC_STEP * HD * 2), "l"(fv), "r"(n) : "memory");
+        }
       }
+      c_k += (size_t)SC_KEYS * HD; c_v += (size_t)SC_KEYS * HD;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");   // (one a step, empty ones too: the count stays)
   };
@@ -144,20 +160,23 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
 #pragma unroll
   for (int i = 0; i < HALVES * 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
   float m_a = -INFINITY, m_z = -INFINITY, l_a = 0.f, l_z = 0.f;
-  float* const sc_a = sc + ((size_t)kh * R_all + va) * ld;
-  float* const sc_z = sc + ((size_t)kh * R_all + vz) * ld;
+  float* sc_a = sc + ((size_t)kh * R_all + va) * ld + k0 + warp * SC_STEP + 2 * t;
+  float* sc_z = sc + ((size_t)kh * R_all + vz) * ld + k0 + warp * SC_STEP + 2 * t;
+  const bool high = v0 + 8 < v1;                           // (the same for the whole CTA)
   auto piece = [&](uint32_t tile, int row, int h, int i) {
     uint4 x;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
                  : "r"(tile + h * (SC_STEP * 128) + row * 128 + ((i ^ (row & 7)) << 4)) : "memory");
     return x;
   };
+  uint32_t r_stage = 0;
   for (int i = 0; i < steps; ++i) {
     const int key0 = k0 + (i * SC_WARPS + warp) * SC_STEP;
     asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 2) : "memory");
     __syncwarp();                                          // (step i is there for all lanes; step i - 1's stage is free)
     copy(i + C::STAGES - 1);
-    const uint32_t kt = ring + (i % C::STAGES) * C::STEP, vt = kt + SC_STEP * HD * 2;
+    const uint32_t kt = ring + r_stage, vt = kt + SC_STEP * HD * 2;
+    r_stage = r_stage + C::STEP == C::STAGES * C::STEP ? 0 : r_stage + C::STEP;
     float s[2][4];
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {
@@ -169,43 +188,69 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
         mma_16816(s[nt], qf[2 * j + 1], kf.z, kf.w);
       }
     }
+    // rows 8 .. 15 of the tile are left out where there are none (one row a stream has as many as its KV heads have query heads)
     float mx_a = -INFINITY, mx_z = -INFINITY;
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int key = key0 + nt * 8 + 2 * t + e;
-        bool see_a = key < k1, see_z = see_a;
-        if (tree && key >= S) { see_a = see_a && ((anc_a >> (key - S)) & 1ull); see_z = see_z && ((anc_z >> (key - S)) & 1ull); }
-        s[nt][e] = see_a ? s[nt][e] * scale_log2 : -INFINITY;
-        s[nt][2 + e] = see_z ? s[nt][2 + e] * scale_log2 : -INFINITY;
-        mx_a = fmaxf(mx_a, s[nt][e]); mx_z = fmaxf(mx_z, s[nt][2 + e]);
-      }
+      for (int e = 0; e < 4; ++e) s[nt][e] *= scale_log2;
+    if (key0 + SC_STEP > k1 || (tree && key0 + SC_STEP > S)) {          // the end of the chunk, or the pass's own rows
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-      const int key = key0 + nt * 8 + 2 * t;
-      if (ok_a) *reinterpret_cast<float2*>(sc_a + key) = make_float2(s[nt][0], s[nt][1]);
-      if (ok_z) *reinterpret_cast<float2*>(sc_z + key) = make_float2(s[nt][2], s[nt][3]);
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int key = key0 + nt * 8 + 2 * t + e;
+          bool see_a = key < k1, see_z = see_a;
+          if (tree && key >= S) { see_a = see_a && ((anc_a >> (key - S)) & 1ull); see_z = see_z && ((anc_z >> (key - S)) & 1ull); }
+          if (!see_a) s[nt][e] = -INFINITY;
+          if (!see_z) s[nt][2 + e] = -INFINITY;
+        }
+    }
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) mx_a = fmaxf(mx_a, fmaxf(s[nt][0], s[nt][1]));
+    if (ok_a) {
+      *reinterpret_cast<float2*>(sc_a) = make_float2(s[0][0], s[0][1]);
+      *reinterpret_cast<float2*>(sc_a + 8) = make_float2(s[1][0], s[1][1]);
+    }
+    sc_a += SC_KEYS;
+    if (high) {
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) mx_z = fmaxf(mx_z, fmaxf(s[nt][2], s[nt][3]));
+      if (ok_z) {
+        *reinterpret_cast<float2*>(sc_z) = make_float2(s[0][2], s[0][3]);
+        *reinterpret_cast<float2*>(sc_z + 8) = make_float2(s[1][2], s[1][3]);
+      }
+      sc_z += SC_KEYS;
     }
 #pragma unroll
     for (int x = 1; x <= 2; x <<= 1) {
       mx_a = fmaxf(mx_a, __shfl_xor_sync(0xffffffffu, mx_a, x));
-      mx_z = fmaxf(mx_z, __shfl_xor_sync(0xffffffffu, mx_z, x));
+      if (high) mx_z = fmaxf(mx_z, __shfl_xor_sync(0xffffffffu, mx_z, x));
     }
-    const float n_a = fmaxf(m_a, mx_a), n_z = fmaxf(m_z, mx_z);
-    const float b_a = n_a == -INFINITY ? 0.f : n_a, b_z = n_z == -INFINITY ? 0.f : n_z;
-    const float c_a = sc_ex2(m_a - b_a), c_z = sc_ex2(m_z - b_z);
-    m_a = n_a; m_z = n_z;
-    l_a *= c_a; l_z *= c_z;
+    if (__any_sync(0xffffffffu, mx_a > m_a || mx_z > m_z)) {             // a new maximum: what there is is scaled down
+      const float n_a = fmaxf(m_a, mx_a), n_z = fmaxf(m_z, mx_z);
+      const float c_a = n_a == -INFINITY ? 1.f : sc_ex2(m_a - n_a), c_z = n_z == -INFINITY ? 1.f : sc_ex2(m_z - n_z);
+      m_a = n_a; m_z = n_z;
+      l_a *= c_a; l_z *= c_z;
 #pragma unroll
-    for (int i = 0; i < HALVES * 8; ++i) { o[i][0] *= c_a; o[i][1] *= c_a; o[i][2] *= c_z; o[i][3] *= c_z; }
-    uint32_t pf[4];
+      for (int i = 0; i < HALVES * 8; ++i) { o[i][0] *= c_a; o[i][1] *= c_a; o[i][2] *= c_z; o[i][3] *= c_z; }
+    }
+    const float b_a = m_a == -INFINITY ? 0.f : m_a;
+    uint32_t pf[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {
-      const float e0 = sc_ex2(s[nt][0] - b_a), e1 = sc_ex2(s[nt][1] - b_a), e2 = sc_ex2(s[nt][2] - b_z), e3 = sc_ex2(s[nt][3] - b_z);
-      l_a += e0 + e1; l_z += e2 + e3;
+      const float e0 = sc_ex2(s[nt][0] - b_a), e1 = sc_ex2(s[nt][1] - b_a);
+      l_a += e0 + e1;
       pf[nt * 2] = h2_as_u32(__floats2half2_rn(e0, e1));   // (weights up to 1 as fp16: half a step of 2^-11 of each)
-      pf[nt * 2 + 1] = h2_as_u32(__floats2half2_rn(e2, e3));
+    }
+    if (high) {
+      const float b_z = m_z == -INFINITY ? 0.f : m_z;
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+        const float e2 = sc_ex2(s[nt][2] - b_z), e3 = sc_ex2(s[nt][3] - b_z);
+        l_z += e2 + e3;
+        pf[nt * 2 + 1] = h2_as_u32(__floats2half2_rn(e2, e3));
+      }
     }
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) {
