@@ -19,8 +19,7 @@
 
 namespace mlora {
 
-constexpr int SC_WARPS = 4, SC_STEP = 16;                  // warps of a CTA, keys of a warp's step
-constexpr int SC_KEYS = SC_WARPS * SC_STEP;                // keys of a CTA's round; chunks are multiples of it
+constexpr int SC_WARPS = 4;
 
 __device__ __forceinline__ float sc_ex2(float x) {
   float y;
@@ -28,17 +27,21 @@ __device__ __forceinline__ float sc_ex2(float x) {
   return y;
 }
 
-// One CTA: 16 query rows of a kv head against a chunk of keys, the warps taking 16 keys in turn, each through a ring of its own
+// One CTA: 16 query rows of a kv head against a chunk of keys, the warps taking 32 keys (16 of 128 features) in turn, each through a ring of its own
 // in shared memory that it fills with 16-byte asynchronous copies (keys past the end as zeros): STAGES - 1 steps ahead, and no warp
 // waits for another before the end.  The pieces of a row lie as with the 128-byte swizzle: piece i of key k at i ^ (k mod 8).
 // From there to the fragments of mma.m16n8k16 with 16-byte reads, free of bank conflicts.  A product does not depend on the
 // order of its features, nor an output on the order of its columns, so both are dealt to suit them:
 //   S:  lane (g, t) holds, of key g, the pieces 2 t + j of each 64 features; a piece feeds two k-steps (q is dealt the same way)
 //   PV: lane (g, t) holds, of keys 2t, 2t + 1, 2t + 8, 2t + 9, piece g of each 64 features; column g of n-tile i is feature 8 g + i
-// Bound by the bytes of K and V: 8 hd16 rows ...
+// Long segments are bound by the bytes of K and V (eight streams of 16384 rows of 8 heads of 128: 93% of the copy rate), short ones by the
+// length of a step's chain: two products with their exponentials between them take 0.6 us whether a step has 16 keys or 32 (heads of 64,
+// eight ragged streams of up to 2048 rows: 14.3 us by 16, 12.3 by 32; at 128 features 32 keys leave an SM one CTA: 12.0 and 14.6 us for
+// 8 x 16 nodes).
 template <int HD> struct ScCfg {
-  static constexpr int STAGES = HD == 64 ? 4 : 3, CTAS = HD == 64 ? 3 : 2;       // ring of a warp; CTAs an SM
-  static constexpr int STEP = 2 * SC_STEP * HD * 2;                              // bytes of a step: 16 keys' K and V
+  static constexpr int KEYS = HD == 64 ? 32 : 16, ROUND = SC_WARPS * KEYS;       // keys of a warp's step, of all warps' (chunks are multiples)
+  static constexpr int STAGES = HD == 64 ? 2 : 3, CTAS = HD == 64 ? 3 : 2;       // ring of a warp; CTAs an SM
+  static constexpr int STEP = 2 * KEYS * HD * 2;                                 // bytes of a step: its K and V
   static constexpr size_t SMEM = (size_t)SC_WARPS * STAGES * STEP;
 };
 
@@ -105,35 +108,35 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
   const uint32_t ring = tc_smem_u32(sc_smem) + warp * C::STAGES * C::STEP;
   constexpr int LPR = HD / 8, RPI = 32 / LPR;              // lanes a row, rows an instruction
   const int c_row = lane / LPR, c_piece = lane % LPR;
-  const int steps = (k1 - k0 - warp * SC_STEP + SC_KEYS - 1) / SC_KEYS;           // (may be negative: none)
-  const size_t c_first = (size_t)(k0 + warp * SC_STEP + c_row) * HD + c_piece * 8;
+  const int steps = (k1 - k0 - warp * C::KEYS + C::ROUND - 1) / C::ROUND;           // (may be negative: none)
+  const size_t c_first = (size_t)(k0 + warp * C::KEYS + c_row) * HD + c_piece * 8;
   const __half *c_k = kb + c_first, *c_v = vb + c_first;
-  uint32_t c_at[SC_STEP / RPI];                            // where the lane's rows go within a step's K
+  uint32_t c_at[C::KEYS / RPI];                            // where the lane's rows go within a step's K
 #pragma unroll
-  for (int r = 0; r < SC_STEP; r += RPI) c_at[r / RPI] = (c_piece >> 3) * (SC_STEP * 128) + (r + c_row) * 128 + (((c_piece & 7) ^ ((r + c_row) & 7)) << 4);
+  for (int r = 0; r < C::KEYS; r += RPI) c_at[r / RPI] = (c_piece >> 3) * (C::KEYS * 128) + (r + c_row) * 128 + (((c_piece & 7) ^ ((r + c_row) & 7)) << 4);
   uint32_t c_stage = 0;
   auto copy = [&](int i) {                                 // step i of this warp (in turn)
     if (i < steps) {
-      const int left = k1 - (k0 + (i * SC_WARPS + warp) * SC_STEP) - c_row;       // the lane's rows from there on
+      const int left = k1 - (k0 + (i * SC_WARPS + warp) * C::KEYS) - c_row;       // the lane's rows from there on
       const uint32_t dst = ring + c_stage;
       c_stage = c_stage + C::STEP == C::STAGES * C::STEP ? 0 : c_stage + C::STEP;
-      if (left + c_row >= SC_STEP) {
+      if (left + c_row >= C::KEYS) {
 #pragma unroll
-        for (int r = 0; r < SC_STEP; r += RPI) {
+        for (int r = 0; r < C::KEYS; r += RPI) {
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c_at[r / RPI]), "l"(c_k + r * HD) : "memory");
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c_at[r / RPI] + SC_STEP * HD * 2), "l"(c_v + r * HD) : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + c_at[r / RPI] + C::KEYS * HD * 2), "l"(c_v + r * HD) : "memory");
         }
       } else {
 #pragma unroll
-        for (int r = 0; r < SC_STEP; r += RPI) {
+        for (int r = 0; r < C::KEYS; r += RPI) {
           const int n = r < left ? 16 : 0;                 // (nothing is read where the count is 0; the address stays in the segment)
           const size_t back = r < left ? (size_t)r * HD : 0;
           const __half *fk = left > 0 ? c_k + back : kb, *fv = left > 0 ? c_v + back : vb;
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + c_at[r / RPI]), "l"(fk), "r"(n) : "memory");
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + c_at[r / RPI] + SC_STEP * HD * 2), "l"(fv), "r"(n) : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + c_at[r / RPI] + C::KEYS * HD * 2), "l"(fv), "r"(n) : "memory");
         }
       }
-      c_k += (size_t)SC_KEYS * HD; c_v += (size_t)SC_KEYS * HD;
+      c_k += (size_t)C::ROUND * HD; c_v += (size_t)C::ROUND * HD;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");   // (one a step, empty ones too: the count stays)
   };
@@ -160,26 +163,26 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
 #pragma unroll
   for (int i = 0; i < HALVES * 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
   float m_a = -INFINITY, m_z = -INFINITY, l_a = 0.f, l_z = 0.f;
-  float* sc_a = sc + ((size_t)kh * R_all + va) * ld + k0 + warp * SC_STEP + 2 * t;
-  float* sc_z = sc + ((size_t)kh * R_all + vz) * ld + k0 + warp * SC_STEP + 2 * t;
+  float* sc_a = sc + ((size_t)kh * R_all + va) * ld + k0 + warp * C::KEYS + 2 * t;
+  float* sc_z = sc + ((size_t)kh * R_all + vz) * ld + k0 + warp * C::KEYS + 2 * t;
   const bool high = v0 + 8 < v1;                           // (the same for the whole CTA)
   auto piece = [&](uint32_t tile, int row, int h, int i) {
     uint4 x;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
-                 : "r"(tile + h * (SC_STEP * 128) + row * 128 + ((i ^ (row & 7)) << 4)) : "memory");
+                 : "r"(tile + h * (C::KEYS * 128) + row * 128 + ((i ^ (row & 7)) << 4)) : "memory");
     return x;
   };
   uint32_t r_stage = 0;
   for (int i = 0; i < steps; ++i) {
-    const int key0 = k0 + (i * SC_WARPS + warp) * SC_STEP;
+    const int key0 = k0 + (i * SC_WARPS + warp) * C::KEYS;
     asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 2) : "memory");
     __syncwarp();                                          // (step i is there for all lanes; step i - 1's stage is free)
     copy(i + C::STAGES - 1);
-    const uint32_t kt = ring + r_stage, vt = kt + SC_STEP * HD * 2;
+    const uint32_t kt = ring + r_stage, vt = kt + C::KEYS * HD * 2;
     r_stage = r_stage + C::STEP == C::STAGES * C::STEP ? 0 : r_stage + C::STEP;
-    float s[2][4];
+    float s[C::KEYS / 8][4];
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
+    for (int nt = 0; nt < C::KEYS / 8; ++nt) {
       s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
       for (int j = 0; j < KP; ++j) {
@@ -191,12 +194,12 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
     // rows 8 .. 15 of the tile are left out where there are none (one row a stream has as many as its KV heads have query heads)
     float mx_a = -INFINITY, mx_z = -INFINITY;
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
+    for (int nt = 0; nt < C::KEYS / 8; ++nt)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[nt][e] *= scale_log2;
-    if (key0 + SC_STEP > k1 || (tree && key0 + SC_STEP > S)) {          // the end of the chunk, or the pass's own rows
+    if (key0 + C::KEYS > k1 || (tree && key0 + C::KEYS > S)) {          // the end of the chunk, or the pass's own rows
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+      for (int nt = 0; nt < C::KEYS / 8; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int key = key0 + nt * 8 + 2 * t + e;
@@ -207,20 +210,20 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
         }
     }
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) mx_a = fmaxf(mx_a, fmaxf(s[nt][0], s[nt][1]));
+    for (int nt = 0; nt < C::KEYS / 8; ++nt) mx_a = fmaxf(mx_a, fmaxf(s[nt][0], s[nt][1]));
     if (ok_a) {
-      *reinterpret_cast<float2*>(sc_a) = make_float2(s[0][0], s[0][1]);
-      *reinterpret_cast<float2*>(sc_a + 8) = make_float2(s[1][0], s[1][1]);
+#pragma unroll
+      for (int nt = 0; nt < C::KEYS / 8; ++nt) *reinterpret_cast<float2*>(sc_a + nt * 8) = make_float2(s[nt][0], s[nt][1]);
     }
-    sc_a += SC_KEYS;
+    sc_a += C::ROUND;
     if (high) {
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) mx_z = fmaxf(mx_z, fmaxf(s[nt][2], s[nt][3]));
+      for (int nt = 0; nt < C::KEYS / 8; ++nt) mx_z = fmaxf(mx_z, fmaxf(s[nt][2], s[nt][3]));
       if (ok_z) {
-        *reinterpret_cast<float2*>(sc_z) = make_float2(s[0][2], s[0][3]);
-        *reinterpret_cast<float2*>(sc_z + 8) = make_float2(s[1][2], s[1][3]);
+#pragma unroll
+        for (int nt = 0; nt < C::KEYS / 8; ++nt) *reinterpret_cast<float2*>(sc_z + nt * 8) = make_float2(s[nt][2], s[nt][3]);
       }
-      sc_z += SC_KEYS;
+      sc_z += C::ROUND;
     }
 #pragma unroll
     for (int x = 1; x <= 2; x <<= 1) {
@@ -236,33 +239,36 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
       for (int i = 0; i < HALVES * 8; ++i) { o[i][0] *= c_a; o[i][1] *= c_a; o[i][2] *= c_z; o[i][3] *= c_z; }
     }
     const float b_a = m_a == -INFINITY ? 0.f : m_a;
-    uint32_t pf[4] = {0u, 0u, 0u, 0u};
+    uint32_t pf[C::KEYS / 16][4] = {};
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
+    for (int nt = 0; nt < C::KEYS / 8; ++nt) {
       const float e0 = sc_ex2(s[nt][0] - b_a), e1 = sc_ex2(s[nt][1] - b_a);
       l_a += e0 + e1;
-      pf[nt * 2] = h2_as_u32(__floats2half2_rn(e0, e1));   // (weights up to 1 as fp16: half a step of 2^-11 of each)
+      pf[nt >> 1][(nt & 1) * 2] = h2_as_u32(__floats2half2_rn(e0, e1));   // (weights up to 1 as fp16: half a step of 2^-11 of each)
     }
     if (high) {
       const float b_z = m_z == -INFINITY ? 0.f : m_z;
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
+      for (int nt = 0; nt < C::KEYS / 8; ++nt) {
         const float e2 = sc_ex2(s[nt][2] - b_z), e3 = sc_ex2(s[nt][3] - b_z);
         l_z += e2 + e3;
-        pf[nt * 2 + 1] = h2_as_u32(__floats2half2_rn(e2, e3));
+        pf[nt >> 1][(nt & 1) * 2 + 1] = h2_as_u32(__floats2half2_rn(e2, e3));
       }
     }
 #pragma unroll
-    for (int h = 0; h < HALVES; ++h) {
-      const uint4 x0 = piece(vt, 2 * t, h, g), x1 = piece(vt, 2 * t + 1, h, g), x2 = piece(vt, 2 * t + 8, h, g), x3 = piece(vt, 2 * t + 9, h, g);
-      const uint32_t w0[4] = {x0.x, x0.y, x0.z, x0.w}, w1[4] = {x1.x, x1.y, x1.z, x1.w};
-      const uint32_t w2[4] = {x2.x, x2.y, x2.z, x2.w}, w3[4] = {x3.x, x3.y, x3.z, x3.w};
+    for (int q = 0; q < C::KEYS / 16; ++q)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        mma_16816(o[h * 8 + 2 * e], pf, __byte_perm(w0[e], w1[e], 0x5410), __byte_perm(w2[e], w3[e], 0x5410));
-        mma_16816(o[h * 8 + 2 * e + 1], pf, __byte_perm(w0[e], w1[e], 0x7632), __byte_perm(w2[e], w3[e], 0x7632));
+      for (int h = 0; h < HALVES; ++h) {
+        const int r = q * 16 + 2 * t;
+        const uint4 x0 = piece(vt, r, h, g), x1 = piece(vt, r + 1, h, g), x2 = piece(vt, r + 8, h, g), x3 = piece(vt, r + 9, h, g);
+        const uint32_t w0[4] = {x0.x, x0.y, x0.z, x0.w}, w1[4] = {x1.x, x1.y, x1.z, x1.w};
+        const uint32_t w2[4] = {x2.x, x2.y, x2.z, x2.w}, w3[4] = {x3.x, x3.y, x3.z, x3.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          mma_16816(o[h * 8 + 2 * e], pf[q], __byte_perm(w0[e], w1[e], 0x5410), __byte_perm(w2[e], w3[e], 0x5410));
+          mma_16816(o[h * 8 + 2 * e + 1], pf[q], __byte_perm(w0[e], w1[e], 0x7632), __byte_perm(w2[e], w3[e], 0x7632));
+        }
       }
-    }
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   __syncthreads();                                         // the rings become the warps' outputs, [SC_WARPS][16][HD]
@@ -869,20 +875,36 @@ cudaError_t init_scored() {
 }
 
 // ----------------------------------------------------------------------------- plan
-// The tcgen05 kernels where a stream has more than 16 rows a KV head and the scores in scratch would be many: from 3 million words on (heads
-// of 64 features; 2.25 of 128), or more than 256 rows that share the prefix.  16 x 32 heads of 64, prefix 512, 64 own keys, one stream
-// (0.3 M words): 9.0 us by the kernels for few rows, 12.9 by these; 8 x 8 x 32 rows, 512 + 1000 keys (3.1 M) 18.0 and 20.5, 2048 + 200 keys
-// (4.6 M) 26.4 and 20.6; 8 x 16 x 32 rows, 512 + 64 keys 27.6 and 17.8; 16 x 6 x 32, no prefix, 100 keys 11.1 and 14.6.
+// Which kernels.  A stream with more than 16 rows a KV head: those for few rows while their scores in scratch are few, up to 3 million
+// words (heads of 64 features; 2.25 of 128) and 256 rows that share the prefix.  16 x 32 heads of 64, prefix 512, 64 own keys, one stream
+// (0.3 M words): 9.0 us by the kernels for few rows, 12.9 by the tcgen05 ones; 8 x 8 x 32 rows, 512 + 1000 keys (3.1 M) 18.0 and 20.5, 2048 +
+// 200 keys (4.6 M) 26.4 and 20.6; 8 x 16 x 32 rows, 512 + 64 keys 27.6 and 17.8; 16 x 6 x 32, no prefix, 100 keys 11.1 and 14.6.
+// Up to 16 rows (decode): the tcgen05 ones only for many streams behind a long prefix, with own segments so short that it does not matter that
+// these fill a few of 128 accumulator columns: 32 streams of 32 heads of 64, 4096 + 200 keys 33.5 and 27.7, 4096 + 1000 keys 35.9 and 42.7,
+// 2048 + 100 keys 21.1 and 21.2; 16 of 24 heads of 128, 2048 + 100 keys 25.4 and 16.5, 512 + 100 keys 12.3 and 13.2.
+static int sc_round(const ScoredArgs& a) { return a.hd == 64 ? ScCfg<64>::ROUND : ScCfg<128>::ROUND; }
 static int sc_resident(const ScoredArgs& a, int sm_count) { return sm_count * (a.hd == 64 ? ScCfg<64>::CTAS : ScCfg<128>::CTAS); }
 static size_t sc_rows(const ScoredArgs& a) { return (size_t)a.n * a.T * a.Hq; }
-static bool sc_tc_shape(const ScoredArgs& a) { const int G = a.Hq / a.Hkv; return a.T * G > 16 && G <= SW_ROWS && tensor_maps_available(); }
-// the longest own segments that the kernels for few rows take where the others could (negative: none)
-static long long sc_few_bound(const ScoredArgs& a, int sm_count) {
+static bool sc_tc_possible(const ScoredArgs& a) {          // at some bound
   const int G = a.Hq / a.Hkv;
-  if ((a.P > 0 && (long long)a.n * a.T * G > 256) || (long long)a.Hkv * a.n * ((a.T * G + 15) / 16) > sc_resident(a, sm_count)) return -1;
-  return (a.hd == 64 ? 3000000ll : 2250000ll) / (long long)sc_rows(a) - a.P - a.T;
+  if (G > SW_ROWS || !tensor_maps_available()) return false;
+  return a.T * G > 16 || ((long long)a.n * a.T * G >= 48 && (long long)sc_rows(a) * a.P >= (a.hd == 64 ? 4000000ll : 750000ll));
 }
-static bool sc_tc(const ScoredArgs& a, int sm_count) { return sc_tc_shape(a) && a.suffix_bound > sc_few_bound(a, sm_count); }
+// where the tcgen05 kernels are possible: the shortest and longest own segments that they take (longest < shortest: none)
+static void sc_tc_bounds(const ScoredArgs& a, int sm_count, long long& lo, long long& hi) {
+  const int G = a.Hq / a.Hkv;
+  lo = 0; hi = 1ll << 40;
+  if (a.T * G <= 16) { hi = 1024ll / ((long long)a.n * a.Hkv) * SW_KEYS - a.T; return; }
+  if ((a.P > 0 && (long long)a.n * a.T * G > 256) || (long long)a.Hkv * a.n * ((a.T * G + 15) / 16) > sc_resident(a, sm_count)) return;
+  const long long few = (a.hd == 64 ? 3000000ll : 2250000ll) / (long long)sc_rows(a) - a.P - a.T;
+  lo = few < 0 ? 0 : few + 1;
+}
+static bool sc_tc(const ScoredArgs& a, int sm_count) {
+  if (!sc_tc_possible(a)) return false;
+  long long lo, hi;
+  sc_tc_bounds(a, sm_count, lo, hi);
+  return a.suffix_bound >= lo && a.suffix_bound <= hi;
+}
 
 // Few rows: the keys in chunks that make one wave of CTAs where that is possible (chunks of at least a round of keys), else
 // four waves.  `work` = keys times 16-row tiles of all KV heads.
@@ -893,9 +915,10 @@ static int sc_chunk(const ScoredArgs& a, int sm_count) {
   const long long resident = sc_resident(a, sm_count), work = sc_work(a), own_keys = (long long)a.suffix_bound + a.T;
   const long long own_items = (long long)a.Hkv * a.n * a.rt_own, prefix_items = a.P > 0 ? (long long)a.Hkv * a.rt_prefix : 0;
   auto up = [](long long x, long long y) { return (x + y - 1) / y; };
-  if (own_items + prefix_items > resident) return (int)(up(work, 4 * resident * SC_KEYS) * SC_KEYS);
-  long long chunk = up(work, resident * SC_KEYS) * SC_KEYS;
-  while (own_items * up(own_keys, chunk) + prefix_items * up(a.P, chunk) > resident) chunk += up(chunk, 16 * SC_KEYS) * SC_KEYS;
+  const long long round = sc_round(a);
+  if (own_items + prefix_items > resident) return (int)(up(work, 4 * resident * round) * round);
+  long long chunk = up(work, resident * round) * round;
+  while (own_items * up(own_keys, chunk) + prefix_items * up(a.P, chunk) > resident) chunk += up(chunk, 16 * round) * round;
   return (int)chunk;
 }
 
@@ -937,8 +960,8 @@ static void sc_plan_few(ScoredArgs& a, int sm_count) {
   a.prefix_chunk = a.own_chunk = chunk;
   a.n_prefix_chunks = (a.P + chunk - 1) / chunk;
   a.n_own_chunks = (int)((own_keys + chunk - 1) / chunk);
-  a.ld_prefix = (a.P + 15) / 16 * 16;
-  a.ld_own = (int)((own_keys + 15) / 16 * 16);
+  a.ld_prefix = (a.P + 31) / 32 * 32;
+  a.ld_own = (int)((own_keys + 31) / 32 * 32);
 }
 
 void scored_plan(ScoredArgs& a, int sm_count) {
@@ -959,27 +982,31 @@ size_t scored_workspace_floats(const ScoredArgs& a) {
   return a.tc ? sw_floats(a, (size_t)a.attn.n_prefix_chunks + a.attn.n_own_chunks) : sc_floats(a);
 }
 
-// Each form needs more for a longer bound.
+// Each form needs more for a longer bound: the longest up to this one that goes by it counts.
 size_t scored_workspace_most(const ScoredArgs& given, int sm_count) {
   ScoredArgs a = given;
   size_t most = 0;
-  long long few = a.suffix_bound;                          // the longest bound up to this one that goes by the kernels for few rows
-  if (sc_tc(a, sm_count)) {
+  long long lo = 1ll << 40, hi = -1;                       // bounds that go by the tcgen05 kernels
+  if (sc_tc_possible(a)) sc_tc_bounds(a, sm_count, lo, hi);
+  if (lo <= given.suffix_bound && lo <= hi) {
+    a.suffix_bound = (int)(hi < given.suffix_bound ? hi : given.suffix_bound);
     // a CTA writes at most 128 rows of partial results; there are no more than four an SM, or one for each item, or one a tile
     const long long items = sw_ctas(a, 1 << 28), all = sw_ctas(a, 1), four = 4ll * sm_count;
     const long long ctas = all < four ? all : (items > four ? items : four);
     most = sw_floats(a, 0) + (size_t)(SW_ROWS * ctas) * (a.hd + 2);
-    few = sc_few_bound(a, sm_count);
-    if (few < 0) return most;
   }
-  a.suffix_bound = (int)few;
-  sc_plan_few(a, sm_count);
-  // a CTA writes 16 rows of partial results; there are never more than four waves of CTAs and one for each item, nor more than
-  // rounds of keys and one for each item (sc_chunk)
-  const long long items = (long long)a.Hkv * ((long long)a.n * a.rt_own + a.rt_prefix);
-  const long long waves = 4ll * sc_resident(a, sm_count), rounds = sc_work(a) / SC_KEYS + 1;
-  const size_t f = (size_t)(16 * ((waves < rounds ? waves : rounds) + items)) * (a.hd + 2) + sc_rows(a) * ((size_t)a.ld_prefix + a.ld_own);
-  return f > most ? f : most;
+  const long long few = given.suffix_bound >= lo && given.suffix_bound <= hi ? lo - 1 : given.suffix_bound;
+  if (few >= 0) {
+    a.suffix_bound = (int)few;
+    sc_plan_few(a, sm_count);
+    // a CTA writes 16 rows of partial results; there are never more than four waves of CTAs and one for each item, nor more than
+    // rounds of keys and one for each item (sc_chunk)
+    const long long items = (long long)a.Hkv * ((long long)a.n * a.rt_own + a.rt_prefix);
+    const long long waves = 4ll * sc_resident(a, sm_count), rounds = sc_work(a) / sc_round(a) + 1;
+    const size_t f = (size_t)(16 * ((waves < rounds ? waves : rounds) + items)) * (a.hd + 2) + sc_rows(a) * ((size_t)a.ld_prefix + a.ld_own);
+    most = f > most ? f : most;
+  }
+  return most;
 }
 
 void scored_carve(ScoredArgs& a, float* ws) {              // ws: 16-byte aligned
