@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) scored_finish_kernel(const Sco
   const int r_step = all_rows ? 1 : FIN_WARPS;
   float x[4 * FIN_FLY];                                    // scores: four keys of FIN_FLY rows, or one key of FIN_ONE rows
   auto fetch = [&](int k0, int r0, int rows, int r) {      // the lane's keys from k0 on, of rows r0 + r, r0 + r + r_step, ...
-    // (a scratch row is a multiple of 16 keys long; what lies past the last key is read and not used)
+    // (a scratch row is a multiple of 32 keys long; what lies past the last key is read and not used)
     const float* const at = sc + ((size_t)kh * R_all + r0) * ld + (one ? min(k0 + lane, ld - 1) : min(k0 + 4 * lane, ld - 4));
     if (one) {
 #pragma unroll
@@ -811,8 +811,8 @@ static cudaError_t sw_launch(const ScoredArgs& a, cudaStream_t st) {
   AttnArgs t = a.attn;
   t.q = a.q; t.prefix_k = a.prefix_k; t.prefix_v = a.prefix_v; t.prefix_head_stride = (size_t)a.P * HD;
   t.own_k = a.own_k; t.own_v = a.own_v; t.own_head_stride = (size_t)a.cap * HD; t.own_stream_stride = t.own_head_stride * a.Hkv;
-  // (its CTAs start while the masks are made; the lengths are the caller's own, for which its chunks and copies stay in bounds whatever they say)
-  t.pdl = 1; t.anc_late = 1; t.suffix_len = a.suffix_len; t.anc = a.anc; t.depth = a.depth; t.out = a.out; t.status = a.status; t.part_o = a.part_o; t.part_ml = a.part_ml;
+  // (its CTAs start while the masks are made)
+  t.pdl = 1; t.anc_late = 1; t.len_limit = a.suffix_bound + 1; t.suffix_len = a.suffix_len; t.anc = a.anc; t.depth = a.depth; t.out = a.out; t.status = a.status; t.part_o = a.part_o; t.part_ml = a.part_ml;
   if ((e = launch_attention(t, st)) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2];

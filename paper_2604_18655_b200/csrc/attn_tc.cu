@@ -90,6 +90,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs p, const int rb_rows, const int 
       it.own = 1; it.slot = p.n_prefix_chunks + chunk; it.s = item / (rb_own * p.n_own_chunks);
       it.v_lo = it.s * p.T * g + rb * NQ * rb_rows; it.v_hi = (it.s + 1) * p.T * g;
       S_own = p.suffix_len[it.s];
+      if (p.len_limit != 0) S_own = max(0, min(S_own, p.len_limit - 1));
       it.k0 = chunk * p.own_chunk; it.k1 = S_own + p.T;
       // (the last chunk takes what is left, whatever bound the chunks were planned with)
       if (chunk + 1 < p.n_own_chunks) it.k1 = min(it.k1, it.k0 + p.own_chunk);

@@ -201,6 +201,7 @@ struct AttnArgs {
   long long* trace0;              // timeline of a traced step (nullptr otherwise): this launch's 12 slots
   int o_direct;                   // o_tabA is indexed by stream (looked up once per call): o_adapter_idx is not read
   int pdl;                        // launch the single-kernel decode attention with programmatic stream serialisation
+  int len_limit;                  // not 0: lengths of own segments are taken as within 0 .. len_limit - 1 (the tcgen05 kernel)
   int anc_late;                   // tree masks are written by the kernel ahead of this programmatic launch (the tcgen05 kernel waits for it)
 };
 

@@ -258,6 +258,22 @@ def test_scored_reports_bad_trees_and_lengths(mb):
         assert int(st.item()) == -1
 
 
+@pytest.mark.parametrize("T", [1, 40])
+def test_scored_takes_lengths_as_within_their_bound(mb, T):
+    """Lengths far outside 0 .. suffix_bound: reported, and the results of the nearest length inside"""
+    n, Hq, Hkv, hd, cap, bound = 4, 8, 2, 64, 400, 300
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v = (torch.randn(*s, generator=g, device="cuda", dtype=torch.float16) for s in ((n * T, Hq, hd), (n, Hkv, cap, hd), (n, Hkv, cap, hd)))
+    ws = torch.empty(mb.mlora_attention_scored_workspace_bytes(n, T, Hq, Hkv, hd, 0, bound), dtype=torch.uint8, device="cuda")
+    res = []
+    for lens, code in (([0, 0, bound, bound], 0), ([-2**31, -5, 2**31 - 1, bound + 1], -1)):
+        out, w, st = torch.zeros_like(q), torch.zeros(n, Hkv, cap, device="cuda"), status()
+        mb.mlora_attention_scored(q, None, None, k, v, i32(lens), bound, None, out, w, None, ws, st)
+        assert int(st.item()) == code
+        res.append((out, w))
+    assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1]) and not res[1][1][:, :, bound + T:].any()
+
+
 def test_scored_large_scores_and_infinite_keys(mb):
     """Scores far apart, a key of -inf features (weight 0 by the softmax itself) and one that takes all the weight."""
     n, Hq, Hkv, hd, cap = 1, 4, 1, 64, 70
