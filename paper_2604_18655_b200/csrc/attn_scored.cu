@@ -325,16 +325,14 @@ __device__ __forceinline__ int sc_slots(const ScoredArgs& p, int s) {
   return p.n_prefix_chunks + min(p.n_own_chunks, (sc_len(p, s) + p.T + p.own_chunk - 1) / p.own_chunk);
 }
 
-// One warp: row w = kv head * R_all + v joined from its slots and written; returns (maximum, 1 / sum).  ns(s): slots that a row of
-// stream s has.
-template <int HD, class F>
-__device__ __forceinline__ float2 sc_join_row(const ScoredArgs& p, int w, int R_all, int slots, int lane, F&& slots_of) {
+// One warp: row w = kv head * R_all + v joined from its first `ns` slots and written; returns (maximum, 1 / sum).
+template <int HD>
+__device__ __forceinline__ float2 sc_join_row(const ScoredArgs& p, int w, int R_all, int slots, int lane, int ns) {
   constexpr int N = HD / 32;                               // features of a lane
   const int G = p.Hq / p.Hkv, kh = w / R_all, v = w - kh * R_all, m = v / G;
   const size_t at = (size_t)w * slots;
   const float2* const ml_at = reinterpret_cast<const float2*>(p.part_ml) + at;
   float M = -INFINITY, L = 0.f, a[N] = {};
-  int ns = slots;
   for (int i0 = 0; i0 < ns; i0 += FIN_FLY) {               // FIN_FLY slots at a time, in order
     float x[FIN_FLY][N];
     float2 ml[FIN_FLY];
@@ -342,13 +340,12 @@ __device__ __forceinline__ float2 sc_join_row(const ScoredArgs& p, int w, int R_
     for (int i = 0; i < FIN_FLY; ++i) {
       const int k = i0 + i;
       ml[i] = make_float2(-INFINITY, 0.f);
-      if (k >= slots) continue;
+      if (k >= slots) continue;                            // (a slot that was not written is read and not used)
       asm volatile("ld.global.cg.v2.f32 {%0, %1}, [%2];" : "=f"(ml[i].x), "=f"(ml[i].y) : "l"(ml_at + k) : "memory");
       const float* po = p.part_o + (at + k) * HD + lane * N;
       if constexpr (N == 4) asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[i][0]), "=f"(x[i][1]), "=f"(x[i][2]), "=f"(x[i][3]) : "l"(po) : "memory");
       else asm volatile("ld.global.cg.v2.f32 {%0, %1}, [%2];" : "=f"(x[i][0]), "=f"(x[i][1]) : "l"(po) : "memory");
     }
-    if (i0 == 0) ns = slots_of(m / p.T);
     float Mn = M;
 #pragma unroll
     for (int i = 0; i < FIN_FLY; ++i) Mn = i0 + i < ns ? fmaxf(Mn, ml[i].x) : Mn;
@@ -375,9 +372,8 @@ __device__ __forceinline__ float2 sc_join_row(const ScoredArgs& p, int w, int R_
 
 // Blocks: rows of the output (one warp a row), then the prefix keys, then the own keys.  Of up to eight rows a warp takes all, for 128
 // keys (four a lane); of more every fourth, for the block's 128 keys, or 32 (one a lane; ONE) where there would be few blocks.
-// Bound by the length of its chain of reads, so everything whose address is known goes out first: partial results
-// and scores before the length, maxima and sums that say what they count for (memory of the workspace in any case, never written
-// in vain).
+// Bound by the length of its chain of reads, so everything that can goes out first: lengths before the kernel ahead has ended, scores before
+// the maxima and sums that say what they count for.
 template <int HD, bool ONE>
 __global__ void __launch_bounds__(FIN_THREADS, 5) scored_finish_kernel(const ScoredArgs p, const int out_blocks, const int prefix_blocks, const int own_blocks,
                                                                     const int prefix_keys, const int own_keys) {
@@ -388,8 +384,9 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) scored_finish_kernel(const Sco
   if (b < out_blocks) {
     const int w = b * FIN_WARPS + warp;
     if (w >= p.Hkv * R_all) return;
+    const int ns = sc_slots(p, w % R_all / R);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    sc_join_row<HD>(p, w, R_all, slots, lane, [&](int s) { return sc_slots(p, s); });
+    sc_join_row<HD>(p, w, R_all, slots, lane, ns);
     return;
   }
   b -= out_blocks;
@@ -412,6 +409,9 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) scored_finish_kernel(const Sco
     limit = sc_len(p, s) + p.T;
     if (key0 >= limit) return;
   }
+  // (the slots of the row that the thread joins first: the lengths are an input)
+  const int r_first = min(FIN_ROWS, v1 - v0) <= 2 * FIN_THREADS / 8 ? tid >> 3 : tid;
+  const int ns_first = sc_slots(p, (v0 + min(r_first, v1 - v0 - 1)) / R);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const bool all_rows = keys > FIN_KEYS, one = ONE && keys < FIN_KEYS;
   const int r_step = all_rows ? 1 : FIN_WARPS;
@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) scored_finish_kernel(const Sco
     constexpr int lanes = decltype(lanes_c)::value, per = FIN_THREADS / lanes;
     const int l = tid & (lanes - 1);
     for (int r = tid / lanes; r < (rows + per - 1) / per * per; r += per) {
-      const int v = r0 + min(r, rows - 1), ns = sc_slots(p, v / R);
+      const int v = r0 + min(r, rows - 1), ns = r0 == v0 && r == r_first ? ns_first : sc_slots(p, v / R);
       const float2* const ml_at = reinterpret_cast<const float2*>(p.part_ml) + ((size_t)kh * R_all + v) * slots;
       float M = -INFINITY, L = 0.f;
 #pragma unroll 4
@@ -552,12 +552,12 @@ constexpr int JOIN_THREADS = 128;
 template <int HD>
 __global__ void __launch_bounds__(JOIN_THREADS) scored_join_kernel(const ScoredArgs p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // (scored_weights_kernel, which waits for this one)
-  const int w = blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31, R_all = p.n * p.T * (p.Hq / p.Hkv);
+  const int w = blockIdx.x * (JOIN_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31, R = p.T * (p.Hq / p.Hkv), R_all = p.n * R;
+  const AttnArgs& t = p.attn;
+  const int ns = w < p.Hkv * R_all ? t.n_prefix_chunks + min(t.n_own_chunks, (sc_len(p, w % R_all / R) + p.T + t.own_chunk - 1) / t.own_chunk) : 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (w >= p.Hkv * R_all) return;
-  const AttnArgs& t = p.attn;
-  const float2 ml = sc_join_row<HD>(p, w, R_all, t.n_prefix_chunks + t.n_own_chunks, lane, [&](int s) {
-    return t.n_prefix_chunks + min(t.n_own_chunks, (sc_len(p, s) + p.T + t.own_chunk - 1) / t.own_chunk); });
+  const float2 ml = sc_join_row<HD>(p, w, R_all, t.n_prefix_chunks + t.n_own_chunks, lane, ns);
   if (lane == 0) p.row_ml[w] = ml;
 }
 

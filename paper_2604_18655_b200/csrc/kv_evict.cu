@@ -269,36 +269,33 @@ __global__ void __launch_bounds__(THREADS) kv_select_kernel(const EvictArgs p, c
     }
   } else {
   // ---- the class in which the order is decided: the new rows where they alone fill the budget, else the others
-  bool among_new = false;
-  int want = B;
-  if (recency) {
-    int mine = 0, n_new;
-    pass([&] { mine += __popc(fresh); });
-    before(__reduce_add_sync(0xffffffffu, mine), n_new);
-    among_new = n_new >= B;
-    want = among_new ? B : B - n_new;                      // rows of the class that stay (may be 0)
-  }
-  const bool none = want == 0;
-  auto of_class = [&] { return among_new ? fresh : there & ~fresh; };
-  // ---- the range of the class's images, then the bin of the want-th largest, again within that bin, ...
+  // -- and the range of all images, in which the histograms start.  One exchange for both.
   uint32_t lo = 0xffffffffu, hi = 0u;
+  int n_new = 0;
   pass([&] {
-    const uint32_t cls = of_class();
+    n_new += __popc(fresh);
 #pragma unroll
     for (int j = 0; j < CH; ++j)
-      if ((cls >> j) & 1u) { lo = min(lo, key[j]); hi = max(hi, key[j]); }
+      if ((there >> j) & 1u) { lo = min(lo, key[j]); hi = max(hi, key[j]); }
   });
-  lo = __reduce_min_sync(0xffffffffu, lo); hi = __reduce_max_sync(0xffffffffu, hi);
-  if (lane == 0) { s_lo[warp] = lo; s_hi[warp] = hi; }
+  lo = __reduce_min_sync(0xffffffffu, lo); hi = __reduce_max_sync(0xffffffffu, hi); n_new = __reduce_add_sync(0xffffffffu, n_new);
+  if (lane == 0) { s_lo[warp] = lo; s_hi[warp] = hi; s_w[0][warp] = n_new; }     // (phase is 0: `before` starts with the other)
   for (int i = tid; i < EV_BINS; i += THREADS) hist[i] = 0;
   __syncthreads();
   lo = __reduce_min_sync(0xffffffffu, s_lo[lane < WARPS ? lane : 0]); hi = __reduce_max_sync(0xffffffffu, s_hi[lane < WARPS ? lane : 0]);
+  n_new = __reduce_add_sync(0xffffffffu, lane < WARPS ? s_w[0][lane] : 0);
   if constexpr (CL) {
-    if (tid == 0) { s_range[0] = lo; s_range[1] = hi; }
+    if (tid == 0) { s_range[0] = lo; s_range[1] = hi; s_cta[0] = n_new; }
     ev_cluster_sync();
     const int c = lane < ctas ? lane : 0;
     lo = __reduce_min_sync(0xffffffffu, ev_remote(&s_range[0], c)); hi = __reduce_max_sync(0xffffffffu, ev_remote(&s_range[1], c));
+    n_new = __reduce_add_sync(0xffffffffu, lane < ctas ? (int)ev_remote(&s_cta[0], lane) : 0);
   }
+  const bool among_new = n_new >= B;
+  int want = among_new ? B : B - n_new;                    // rows of the class that stay (may be 0)
+  const bool none = want == 0;
+  auto of_class = [&] { return among_new ? fresh : there & ~fresh; };
+  // ---- the bin of the want-th largest of the class, again within that bin, ...
   bool all_equal_stay = none;                              // the rows at `lo` all stay: nothing to count among them
   if (tid == 0) s_got[0] = s_got[1] = s_got[2] = 0;
   // (three rounds at most; the bound, and those on the list below, hold even if another stream writes the totals meanwhile)

@@ -44,7 +44,7 @@ __device__ __forceinline__ uint4 rope_pack(const float (&f)[8]) {
 
 // An item is 16 features of a head: two pieces of 8 that hold the two halves of 8 pairs (half-split), or 16 neighbours.  Which 16 is
 // fixed for a thread; it goes through the CTA's (row, head) in steps of ROPE_THREADS / items-of-a-head, without divisions, FLY items' reads
-// on their way at a time, the first before the table is filled.  Addresses of the rows come from shared memory.
+// on their way at a time, the first before the table is filled.  Addresses of several rows come from shared memory.
 template <bool F32, int HD, int ROWS, int FLY>
 __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopeArgs p) {
   constexpr int IH = HD / 16, STEP = ROPE_THREADS / IH, SIZE = F32 ? 4 : 2;
@@ -53,12 +53,13 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopeArg
   __shared__ __half* s_dst[ROWS][3];                       // where they go: head 0 of q_out's row, of its place in the own segments; null: nowhere
   const int tid = threadIdx.x, rows = p.n * p.T, row0 = blockIdx.x * ROWS, half = p.rotary >> 1;
   const int H = p.Hq + 2 * p.Hkv, in_rows = min(ROWS, rows - row0);
-  for (int i = tid; i < in_rows * 3; i += ROPE_THREADS) {
-    const int r = i / 3, what = i - r * 3, row = row0 + r;
+  auto row_of = [&](int x, int what) {
     const long long stride = what == 0 ? p.q_stride : (what == 1 ? p.k_stride : p.v_stride);
     const void* base = what == 0 ? p.q : (what == 1 ? p.k : p.v);
-    s_src[r][what] = reinterpret_cast<const unsigned char*>(base) + row * stride * SIZE;
-  }
+    return reinterpret_cast<const unsigned char*>(base) + (row0 + x) * stride * SIZE;
+  };
+  if constexpr (ROWS > 1)
+    for (int i = tid; i < in_rows * 3; i += ROPE_THREADS) s_src[i / 3][i % 3] = row_of(i / 3, i % 3);
   const int it = tid % IH;
   const bool in_turn = it * 16 < p.rotary, split = in_turn && !p.interleaved;
   const int o0 = split ? it * 8 : it * 16, o1 = split ? o0 + half : o0 + 8;      // offsets of the two pieces (v: split is undone below)
@@ -78,13 +79,13 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopeArg
       fr[f] = r; fh[f] = h;
       if (r < in_rows) {
         const int what = (h >= p.Hq) + (h >= p.Hq + p.Hkv), hh = h - (what == 0 ? 0 : (what == 1 ? p.Hq : p.Hq + p.Hkv));
-        const unsigned char* src = s_src[r][what];
+        const unsigned char* src = ROWS == 1 ? row_of(0, what) : s_src[r][what];
         va[f].load(src, hh * HD + (what == 2 ? v0 : o0)); vb[f].load(src, hh * HD + (what == 2 ? v0 + 8 : o1));
       }
       advance(r, h);
     }
   };
-  __syncthreads();
+  if constexpr (ROWS > 1) __syncthreads();
   fetch();
   for (int i = ROPE_THREADS - 1 - tid; i < in_rows * 3; i += ROPE_THREADS) {
     const int x = i / 3, what = i - x * 3, row = row0 + x;
