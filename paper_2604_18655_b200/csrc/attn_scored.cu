@@ -906,20 +906,23 @@ static bool sc_tc(const ScoredArgs& a, int sm_count) {
   return a.suffix_bound >= lo && a.suffix_bound <= hi;
 }
 
-// Few rows: the keys in chunks that make one wave of CTAs where that is possible (chunks of at least a round of keys), else
-// four waves.  `work` = keys times 16-row tiles of all KV heads.
-static long long sc_work(const ScoredArgs& a) {
-  return a.Hkv * (a.rt_prefix * (long long)a.P + (long long)a.n * a.rt_own * ((long long)a.suffix_bound + a.T));
+// Few rows: the keys in chunks of m rounds, m by a CTA's time (half a microsecond a round, four rounds' worth of fixed cost) and the waves
+// that all CTAs make.
+static long long sc_ctas(const ScoredArgs& a, long long chunk) {
+  auto up = [](long long x, long long y) { return (x + y - 1) / y; };
+  return a.Hkv * (a.rt_prefix * up(a.P, chunk) + a.n * (long long)a.rt_own * up((long long)a.suffix_bound + a.T, chunk));
 }
 static int sc_chunk(const ScoredArgs& a, int sm_count) {
-  const long long resident = sc_resident(a, sm_count), work = sc_work(a), own_keys = (long long)a.suffix_bound + a.T;
-  const long long own_items = (long long)a.Hkv * a.n * a.rt_own, prefix_items = a.P > 0 ? (long long)a.Hkv * a.rt_prefix : 0;
-  auto up = [](long long x, long long y) { return (x + y - 1) / y; };
-  const long long round = sc_round(a);
-  if (own_items + prefix_items > resident) return (int)(up(work, 4 * resident * round) * round);
-  long long chunk = up(work, resident * round) * round;
-  while (own_items * up(own_keys, chunk) + prefix_items * up(a.P, chunk) > resident) chunk += up(chunk, 16 * round) * round;
-  return (int)chunk;
+  const long long resident = sc_resident(a, sm_count), round = sc_round(a), own_keys = (long long)a.suffix_bound + a.T;
+  const long long most = ((a.P > own_keys ? a.P : own_keys) + round - 1) / round;
+  long long best = most, cost = -1;
+  for (long long m = most; m >= 1; m -= 1 + m / 16) {
+    const long long ctas = sc_ctas(a, m * round);
+    if (m < most && ctas > 4 * resident) break;
+    const long long c = (ctas + resident - 1) / resident * (4 + m);
+    if (cost < 0 || c <= cost) { cost = c; best = m; }
+  }
+  return (int)(best * round);
 }
 
 // Many rows: prefix and own segments in chunks of at most `m` tiles of 128 keys, m by a CTA's time (about 2 us a tile and two and a
@@ -999,11 +1002,10 @@ size_t scored_workspace_most(const ScoredArgs& given, int sm_count) {
   if (few >= 0) {
     a.suffix_bound = (int)few;
     sc_plan_few(a, sm_count);
-    // a CTA writes 16 rows of partial results; there are never more than four waves of CTAs and one for each item, nor more than
-    // rounds of keys and one for each item (sc_chunk)
-    const long long items = (long long)a.Hkv * ((long long)a.n * a.rt_own + a.rt_prefix);
-    const long long waves = 4ll * sc_resident(a, sm_count), rounds = sc_work(a) / sc_round(a) + 1;
-    const size_t f = (size_t)(16 * ((waves < rounds ? waves : rounds) + items)) * (a.hd + 2) + sc_rows(a) * ((size_t)a.ld_prefix + a.ld_own);
+    // a CTA writes 16 rows of partial results; there are no more than four waves of CTAs, or one for each item, or one for each round
+    const long long items = sc_ctas(a, 1ll << 40), all = sc_ctas(a, sc_round(a)), four = 4ll * sc_resident(a, sm_count);
+    const long long ctas = all < four ? all : (items > four ? items : four);
+    const size_t f = (size_t)(16 * ctas) * (a.hd + 2) + sc_rows(a) * ((size_t)a.ld_prefix + a.ld_own);
     most = f > most ? f : most;
   }
   return most;
@@ -1033,9 +1035,10 @@ static cudaError_t sc_launch(const ScoredArgs& a, cudaStream_t st) {
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   const int out_blocks = (a.n * a.T * a.Hq + FIN_WARPS - 1) / FIN_WARPS;
-  // keys of a block, and blocks: one for all keys only as far as that fills the machine, the rest in turns
+  // keys of a block (32 where 128 would leave SMs idle: 8 x 16 rows 512 + 64 keys 16.7 and 13.5 us with 128 and 32, but one row of eight streams
+  // behind 4096 keys 10.9 and 14.7), and blocks: one for all keys only as far as that fills the machine, the rest in turns
   auto keys_of = [](long long keys, long long segments, int rows) {
-    return rows <= FIN_FLY ? FIN_WARPS * FIN_KEYS : (segments * ((keys + FIN_KEYS - 1) / FIN_KEYS) < 2 * 148 ? 32 : FIN_KEYS);
+    return rows <= FIN_FLY ? FIN_WARPS * FIN_KEYS : (segments * ((keys + FIN_KEYS - 1) / FIN_KEYS) < 148 ? 32 : FIN_KEYS);
   };
   auto blocks_of = [](long long keys, long long segments, int per) {
     const long long all = (keys + per - 1) / per, fill = (148 * 16 + segments - 1) / segments;
