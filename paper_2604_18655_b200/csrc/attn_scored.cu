@@ -876,27 +876,28 @@ cudaError_t init_scored() {
 
 // ----------------------------------------------------------------------------- plan
 // Which kernels.  A stream with more than 16 rows a KV head: those for few rows while their scores in scratch are few, up to 3 million
-// words (heads of 64 features; 2.25 of 128) and 256 rows that share the prefix.  16 x 32 heads of 64, prefix 512, 64 own keys, one stream
-// (0.3 M words): 9.0 us by the kernels for few rows, 12.9 by the tcgen05 ones; 8 x 8 x 32 rows, 512 + 1000 keys (3.1 M) 18.0 and 20.5, 2048 +
-// 200 keys (4.6 M) 26.4 and 20.6; 8 x 16 x 32 rows, 512 + 64 keys 27.6 and 17.8; 16 x 6 x 32, no prefix, 100 keys 11.1 and 14.6.
-// Up to 16 rows (decode): the tcgen05 ones only for many streams behind a long prefix, with own segments so short that it does not matter that
-// these fill a few of 128 accumulator columns: 32 streams of 32 heads of 64, 4096 + 200 keys 33.5 and 27.7, 4096 + 1000 keys 35.9 and 42.7,
-// 2048 + 100 keys 21.1 and 21.2; 16 of 24 heads of 128, 2048 + 100 keys 25.4 and 16.5, 512 + 100 keys 12.3 and 13.2.
+// words (heads of 64 features; 0.85 of 128), and up to 256 rows share the prefix.  Few rows / tcgen05, us: heads of 64, 16 nodes of one
+// stream, 512 + 64 keys (0.3 M words) 8.2 / 10.5, 8 x 8 nodes, 512 + 1000 keys (3.1 M) 17.8 / 18.3, 2048 + 200 keys (4.6 M) 25.0 / 19.2, 8 x 16
+// nodes, 512 + 64 keys (512 rows) 24.0 / 16.2, 16 x 6 nodes, no prefix 11.1 / 12.3; heads of 128, 4 x 8 nodes, 512 + 64 keys (0.4 M) 11.5 / 12.2,
+// 8 x 8 (0.9 M) 19.9 / 14.8.
+// Up to 16 rows (decode): the tcgen05 ones only for many streams behind a long prefix with own segments so short that it does not matter that
+// these fill a few of 128 accumulator columns.  Heads of 64: 32 streams, 8192 + 100 keys (8.4 M words of prefix) 42.4 / 30.7, 16 streams (4.2 M)
+// 22.1 / 25.8, 64 streams, 8192 + 500 keys 68.2 / 68.4; heads of 128: 32 streams, 4096 + 100 keys (3.1 M) 37.6 / 27.6, 4096 + 1000 keys 47.0 / 50.6.
 static int sc_round(const ScoredArgs& a) { return a.hd == 64 ? ScCfg<64>::ROUND : ScCfg<128>::ROUND; }
 static int sc_resident(const ScoredArgs& a, int sm_count) { return sm_count * (a.hd == 64 ? ScCfg<64>::CTAS : ScCfg<128>::CTAS); }
 static size_t sc_rows(const ScoredArgs& a) { return (size_t)a.n * a.T * a.Hq; }
 static bool sc_tc_possible(const ScoredArgs& a) {          // at some bound
   const int G = a.Hq / a.Hkv;
   if (G > SW_ROWS || !tensor_maps_available()) return false;
-  return a.T * G > 16 || ((long long)a.n * a.T * G >= 48 && (long long)sc_rows(a) * a.P >= (a.hd == 64 ? 4000000ll : 750000ll));
+  return a.T * G > 16 || ((long long)a.n * a.T * G >= 48 && (long long)sc_rows(a) * a.P >= (a.hd == 64 ? 6000000ll : 2500000ll));
 }
 // where the tcgen05 kernels are possible: the shortest and longest own segments that they take (longest < shortest: none)
 static void sc_tc_bounds(const ScoredArgs& a, int sm_count, long long& lo, long long& hi) {
   const int G = a.Hq / a.Hkv;
   lo = 0; hi = 1ll << 40;
-  if (a.T * G <= 16) { hi = 1024ll / ((long long)a.n * a.Hkv) * SW_KEYS - a.T; return; }
+  if (a.T * G <= 16) { hi = 512ll / ((long long)a.n * a.Hkv) * SW_KEYS - a.T; return; }
   if ((a.P > 0 && (long long)a.n * a.T * G > 256) || (long long)a.Hkv * a.n * ((a.T * G + 15) / 16) > sc_resident(a, sm_count)) return;
-  const long long few = (a.hd == 64 ? 3000000ll : 2250000ll) / (long long)sc_rows(a) - a.P - a.T;
+  const long long few = (a.hd == 64 ? 3000000ll : 850000ll) / (long long)sc_rows(a) - a.P - a.T;
   lo = few < 0 ? 0 : few + 1;
 }
 static bool sc_tc(const ScoredArgs& a, int sm_count) {

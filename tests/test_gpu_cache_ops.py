@@ -573,7 +573,7 @@ def test_offsets_beyond_32_bits(mb):
     assert torch.equal(src[1, 8].long(), ref) and torch.equal(k[1, 8, :B], kh[ref]) and torch.equal(v[1, 8, :B], vh[ref])
 
 
-@pytest.mark.parametrize("n,T,Hq,Hkv,hd,P,bound", [(2, 1, 8, 2, 64, 100, 3000), (20, 1, 24, 8, 128, 2048, 2500), (2, 9, 32, 8, 64, 700, 1500), (3, 20, 6, 2, 128, 64, 700), (1, 64, 16, 1, 64, 0, 9000)])
+@pytest.mark.parametrize("n,T,Hq,Hkv,hd,P,bound", [(2, 1, 8, 2, 64, 100, 3000), (20, 1, 24, 8, 128, 5500, 2500), (2, 9, 32, 8, 64, 700, 1500), (3, 20, 6, 2, 128, 64, 700), (1, 64, 16, 1, 64, 0, 9000)])
 def test_scored_workspace_serves_every_smaller_bound(mb, n, T, Hq, Hkv, hd, P, bound):
     """One workspace of the largest bound's size, filled with NaN; the call sizes its chunks (and picks its kernels) by each bound."""
     g = torch.Generator(device="cuda").manual_seed(0)
@@ -609,6 +609,7 @@ def test_evict_few_rows_too_many_in_every_place(mb):
 
 def test_scored_many_streams_behind_a_long_prefix(mb):
     """One row a stream, by the tensor-memory kernels where prefix rows are many and own segments short, by the others around that"""
-    scored_case(mb, 34, 1, 16, 4, 128, 2050, [(7 * i) % 100 for i in range(34)], seed=5)
-    scored_case(mb, 32, 1, 32, 8, 64, 4096, [(13 * i) % 130 for i in range(32)], seed=6)
-    scored_case(mb, 32, 1, 32, 8, 64, 4096, [0] * 31 + [700], seed=7, bound=900, slack=300)
+    scored_case(mb, 34, 1, 16, 4, 128, 5000, [(7 * i) % 100 for i in range(34)], seed=5)
+    scored_case(mb, 32, 1, 32, 8, 64, 6001, [(13 * i) % 130 for i in range(32)], seed=6)
+    scored_case(mb, 32, 1, 32, 8, 64, 6001, [0] * 31 + [700], seed=7, bound=900, slack=300)
+    scored_case(mb, 34, 1, 16, 4, 128, 2050, [(7 * i) % 100 for i in range(34)], seed=8)
