@@ -1039,7 +1039,7 @@ static cudaError_t sc_launch(const ScoredArgs& a, cudaStream_t st) {
   // keys of a block (32 where 128 would leave SMs idle: 8 x 16 rows 512 + 64 keys 16.7 and 13.5 us with 128 and 32, but one row of eight streams
   // behind 4096 keys 10.9 and 14.7), and blocks: one for all keys only as far as that fills the machine, the rest in turns
   auto keys_of = [](long long keys, long long segments, int rows) {
-    return rows <= FIN_FLY ? FIN_WARPS * FIN_KEYS : (segments * ((keys + FIN_KEYS - 1) / FIN_KEYS) < 148 ? 32 : FIN_KEYS);
+    return rows <= FIN_FLY ? FIN_WARPS * FIN_KEYS : (segments * ((keys + FIN_KEYS - 1) / FIN_KEYS) < 100 ? 32 : FIN_KEYS);
   };
   auto blocks_of = [](long long keys, long long segments, int per) {
     const long long all = (keys + per - 1) / per, fill = (148 * 16 + segments - 1) / segments;
