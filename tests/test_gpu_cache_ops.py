@@ -613,3 +613,96 @@ def test_scored_many_streams_behind_a_long_prefix(mb):
     scored_case(mb, 32, 1, 32, 8, 64, 6001, [(13 * i) % 130 for i in range(32)], seed=6)
     scored_case(mb, 32, 1, 32, 8, 64, 6001, [0] * 31 + [700], seed=7, bound=900, slack=300)
     scored_case(mb, 34, 1, 16, 4, 128, 2050, [(7 * i) % 100 for i in range(34)], seed=8)
+
+
+@pytest.mark.parametrize("n,T,Hq,Hkv,hd,P,lens", [(4, 32, 32, 8, 64, 1000, [700, 3, 1023, 512]), (3, 60, 24, 8, 128, 300, [500, 0, 129]), (32, 1, 32, 8, 64, 6001, list(range(32)))])
+def test_scored_large_passes_replayed_from_two_graphs(mb, n, T, Hq, Hkv, hd, P, lens):
+    """Passes of the tensor-memory kernels, captured twice with a workspace each and replayed side by side: the bits of direct calls"""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    r16 = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=torch.float16)  # noqa: E731
+    bound = max(lens)
+    cap = bound + T + 5
+    pk, pv, k, v = r16(Hkv, P, hd), r16(Hkv, P, hd), r16(n, Hkv, cap, hd), r16(n, Hkv, cap, hd)
+    par, dl, qs = i32([tree(np.random.default_rng(T), T)] * n), i32(lens), [r16(n * T, Hq, hd) for _ in range(3)]
+    need = mb.mlora_attention_scored_workspace_bytes(n, T, Hq, Hkv, hd, P, bound)
+
+    def make():
+        return dict(q=torch.empty_like(qs[0]), out=torch.empty_like(qs[0]), w=torch.zeros(n, Hkv, cap, device="cuda"), pw=torch.zeros(Hkv, P, device="cuda"),
+                    ws=torch.empty(need, dtype=torch.uint8, device="cuda"), st=status())
+
+    def call(s):
+        mb.mlora_attention_scored(s["q"], pk, pv, k, v, dl, bound, par, s["out"], s["w"], s["pw"], s["ws"], s["st"])
+
+    direct, outs = make(), []
+    for q in qs:
+        direct["q"].copy_(q)
+        call(direct)
+        outs.append(direct["out"].clone())
+    states, graphs, streams = [make(), make()], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in states:
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            call(s)
+        graphs.append(gr)
+    torch.cuda.synchronize()
+    for i, q in enumerate(qs):
+        for s, gr, sm in zip(states, graphs, streams):
+            with torch.cuda.stream(sm):
+                s["q"].copy_(q)
+                gr.replay()
+        torch.cuda.synchronize()
+        for s in states:
+            assert torch.equal(s["out"], outs[i])
+    for s in states:
+        assert torch.equal(s["w"], direct["w"]) and torch.equal(s["pw"], direct["pw"]) and int(s["st"].item()) == 0
+
+
+def test_two_loops_on_two_streams_at_once(mb):
+    """Nothing is shared between calls: steps of two loops enqueued alternately on two streams, against each alone"""
+    n, T, Hq, Hkv, hd, P, B = 4, 3, 8, 2, 128, 200, 300
+    xs = rows(7, 10, n, T, (Hq + 2 * Hkv) * hd)
+    want = []
+    for seed in (1, 2):
+        lp = Loop(mb, n, T, Hq, Hkv, hd, P, B, 20, seed=seed, kept=B - 4)
+        for x in xs:
+            lp.step(*split(x, Hq, Hkv, hd))
+        want.append(lp.state())
+    torch.cuda.synchronize()
+    loops = [Loop(mb, n, T, Hq, Hkv, hd, P, B, 20, seed=seed, kept=B - 4) for seed in (1, 2)]
+    streams = [torch.cuda.Stream() for _ in loops]
+    torch.cuda.synchronize()
+    for x in xs:
+        for lp, sm in zip(loops, streams):
+            with torch.cuda.stream(sm):
+                lp.step(*split(x, Hq, Hkv, hd))
+    torch.cuda.synchronize()
+    for lp, w in zip(loops, want):
+        assert all(torch.equal(a, b) for a, b in zip(lp.state(), w))
+
+
+def test_evict_long_segments_replayed_from_a_graph(mb):
+    """A cluster's selection and the kernel that moves the rows, captured: two replays after one another cut once and then nothing"""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    n, Hkv, hd, S, B = 2, 2, 64, 50000, 20000
+    k, v = (torch.randn(n, Hkv, S, hd, generator=g, device="cuda", dtype=torch.float16) for _ in range(2))
+    w = torch.rand(n, Hkv, S, generator=g, device="cuda")
+    k0, w0 = k.clone(), w.cpu().numpy()
+    lens, ol, st = i32([S, S - 777]), i32([0, 0]), status()
+    src = torch.full((n, Hkv, B), -1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(mb.mlora_kv_evict_workspace_bytes(n, Hkv, S, B), dtype=torch.uint8, device="cuda")
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        mb.mlora_kv_evict(k, v, w, None, lens, S, None, B, 0, w, None, ol, ws, st, out_source=src)
+        lens.copy_(ol)
+    gr.replay()
+    torch.cuda.synchronize()
+    kept = src.clone()
+    for s, m in ((0, S), (1, S - 777)):
+        for h in range(Hkv):
+            want = evict_reference(w0[s, h], np.zeros(S), m, B, 0, 0)
+            assert np.array_equal(kept[s, h].cpu().numpy(), want) and torch.equal(k[s, h, :B], k0[s, h][dev(want)])
+    k1 = k.clone()
+    gr.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(k, k1) and lens.tolist() == [B, B] and torch.equal(src, torch.arange(B, dtype=torch.int32, device="cuda").expand(n, Hkv, B))
+    assert int(st.item()) == 0
