@@ -1042,7 +1042,7 @@ static cudaError_t sc_launch(const ScoredArgs& a, cudaStream_t st) {
     return rows <= FIN_FLY ? FIN_WARPS * FIN_KEYS : (segments * ((keys + FIN_KEYS - 1) / FIN_KEYS) < 100 ? 32 : FIN_KEYS);
   };
   auto blocks_of = [](long long keys, long long segments, int per) {
-    const long long all = (keys + per - 1) / per, fill = (148 * 16 + segments - 1) / segments;
+    const long long all = (keys + per - 1) / per, fill = (148 * 8 + segments - 1) / segments;
     return (int)(all < fill ? all : fill);
   };
   const int G = a.Hq / a.Hkv, own_all = a.suffix_bound + a.T;
