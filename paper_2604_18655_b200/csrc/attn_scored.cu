@@ -412,8 +412,15 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) scored_finish_kernel(const Sco
   // (the slots of the row that the thread joins first: the lengths are an input)
   const int r_first = min(FIN_ROWS, v1 - v0) <= 2 * FIN_THREADS / 8 ? tid >> 3 : tid;
   const int ns_first = sc_slots(p, (v0 + min(r_first, v1 - v0 - 1)) / R);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
   const bool all_rows = keys > FIN_KEYS, one = ONE && keys < FIN_KEYS;
+  // (and so are the totals of a warp's first keys, where every warp has its own: 0.2 us of 5.3 for a single stream, 0.6 of 45.6 for sixteen)
+  float old4[4];
+  auto totals = [&](int k) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) old4[i] = k + i < limit ? dst[k + i] : 0.f;
+  };
+  if (all_rows) totals(key0 + warp * FIN_KEYS + 4 * lane);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int r_step = all_rows ? 1 : FIN_WARPS;
   float x[4 * FIN_FLY];                                    // scores: four keys of FIN_FLY rows, or one key of FIN_ONE rows
   auto fetch = [&](int k0, int r0, int rows, int r) {      // the lane's keys from k0 on, of rows r0 + r, r0 + r + r_step, ...
@@ -468,10 +475,8 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) scored_finish_kernel(const Sco
     __syncthreads();
     for (int k0 = mine; k0 < limit; k0 += step) {
       const int k = k0 + 4 * lane;
-      if (k0 != mine) fetch(k0, v0, rows, 0);
-      float old[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) old[i] = k + i < limit ? dst[k + i] : 0.f;
+      if (k0 != mine) { fetch(k0, v0, rows, 0); totals(k); }
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < FIN_FLY; ++i)
         if (i < rows) {
@@ -481,7 +486,7 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) scored_finish_kernel(const Sco
         }
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (k + i < limit) dst[k + i] = old[i] + sum[i];
+        if (k + i < limit) dst[k + i] = old4[i] + sum[i];
     }
     return;
   }
