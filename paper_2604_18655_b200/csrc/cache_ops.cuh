@@ -60,6 +60,7 @@ struct EvictArgs {
   int32_t* counts;                 // scratch: [n * Hkv] moves
   int2* moves;                     // scratch: [n * Hkv][max_moves] (from, to)
   int max_moves;
+  int past_l2;                     // set by launch_kv_evict: the rows that move may not fit in L2
   int* status;
 };
 cudaError_t launch_kv_evict(const EvictArgs& a, cudaStream_t st);

@@ -26,7 +26,9 @@ __device__ __forceinline__ uint32_t ev_image(float w) {
   return (w != w) ? 0u : ((b & 0x80000000u) ? ~b : (b | 0x80000000u));
 }
 
-// 16 bytes a lane; HD / 8 lanes move a K row, as many its V row; FLY rows on their way at a time
+// 16 bytes a lane; HD / 8 lanes move a K row, as many its V row; FLY rows on their way at a time.  What is written is marked to leave L2
+// first -- the few rows of a stream at its budget excepted -- and so is what is read where L2 cannot hold the moves: 64 segments 16384 ->
+// 8192 rows of 64 features 43.1 us, writes alone marked 55.1, reads alone 52.9, neither 55.4; 32 segments 30.7, 28.8, 29.9 and 32.8.
 template <int HD, int FLY>
 __device__ __forceinline__ void ev_move(const EvictArgs& p, const int2* list, int count, int pair, int first, int step, int l) {
   constexpr int LANES = HD / 4;
@@ -51,14 +53,16 @@ __device__ __forceinline__ void ev_move(const EvictArgs& p, const int2* list, in
 #pragma unroll
     for (int f = 0; f < FLY; ++f) {
       if (m[f].x < 0) continue;
-      x[f] = __ldcs(reinterpret_cast<const uint4*>(c + (size_t)m[f].x * HD));
+      const uint4* const row = reinterpret_cast<const uint4*>(c + (size_t)m[f].x * HD);
+      x[f] = p.past_l2 ? __ldcs(row) : *row;
       side[f] = from != nullptr ? from[m[f].x] : (uint32_t)m[f].x;
     }
     ahead(j + FLY * step);
 #pragma unroll
     for (int f = 0; f < FLY; ++f) {
       if (m[f].x < 0) continue;
-      *reinterpret_cast<uint4*>(c + (size_t)m[f].y * HD) = x[f];
+      if constexpr (FLY == 1) *reinterpret_cast<uint4*>(c + (size_t)m[f].y * HD) = x[f];
+      else __stcs(reinterpret_cast<uint4*>(c + (size_t)m[f].y * HD), x[f]);
       if (to != nullptr) to[m[f].y] = side[f];
     }
   }
@@ -458,11 +462,15 @@ static cudaError_t ev_select(const EvictArgs& a, int ctas, int move_here, cudaSt
   return cudaLaunchKernelEx(&cfg, kv_select_kernel<THREADS, KPT, CL, FEW>, a, move_here);
 }
 
-cudaError_t launch_kv_evict(const EvictArgs& a, cudaStream_t st) {
+cudaError_t launch_kv_evict(const EvictArgs& args, cudaStream_t st) {
+  EvictArgs a = args;
   // The selecting CTAs move the rows themselves where these are few, or where the segments fill the SMs (one CTA each) to 60% in every
   // wave: 256 segments 4096 -> 2048 rows 38.9 us, 43.0 by a kernel of their own; 160 segments 30.9 and 28.7, 16 segments 16.4 and 11.6.
   const int pairs = a.n * a.Hkv, waves = (pairs + 147) / 148;
   const int move_here = a.max_moves <= 256 || pairs * 5 >= waves * 148 * 3;
+  // About half of the worst case moves, from somewhere to somewhere else: as many bytes as this, of 126 MB.  (67 and 84 MB gain by keeping
+  // what is read, 134 MB lose.)
+  a.past_l2 = (size_t)pairs * a.max_moves * a.hd * 4 > 100000000;
   const bool few = a.bound - a.budget <= EV_FEW;           // (one row of 257 in eight segments: 2.9 us, 4.3 by histograms)
   cudaError_t e;
   if (few && a.bound <= 1024) e = ev_select<256, 4, false, true>(a, 1, move_here, st);
@@ -478,7 +486,9 @@ cudaError_t launch_kv_evict(const EvictArgs& a, cudaStream_t st) {
   if (e != cudaSuccess || move_here) return e;
   cudaLaunchConfig_t cfg{};
   const int per = 4 * (256 / (a.hd / 4)), most = (a.max_moves + per - 1) / per;
-  const int want = (2 * 148 * 8 + pairs - 1) / pairs;
+  // (as many CTAs as fit, 32 segments 8192 -> 4096 rows 15.4 and 16.8 us by twice as many; twice as many past L2, 64 segments 16384 ->
+  // 8192 rows 41.6 and 42.9)
+  const int want = ((a.past_l2 ? 2 : 1) * 148 * 8 + pairs - 1) / pairs;
   cfg.gridDim = dim3((unsigned)(most < want ? most : want), (unsigned)pairs);
   cfg.blockDim = dim3(256); cfg.stream = st;
   cudaLaunchAttribute attr[1];
