@@ -465,7 +465,8 @@ static cudaError_t ev_select(const EvictArgs& a, int ctas, int move_here, cudaSt
 cudaError_t launch_kv_evict(const EvictArgs& args, cudaStream_t st) {
   EvictArgs a = args;
   // The selecting CTAs move the rows themselves where these are few, or where the segments fill the SMs (one CTA each) to 60% in every
-  // wave: 256 segments 4096 -> 2048 rows 38.9 us, 43.0 by a kernel of their own; 160 segments 30.9 and 28.7, 16 segments 16.4 and 11.6.
+  // wave: 256 segments 4096 -> 2048 rows 36.9 us, 40.6 by a kernel of their own (96 segments 14.6 and 15.2 in a graph; 160 segments 30.9 and 28.7,
+  // 16 segments 16.4 and 11.6; of 128 segments with 128 features and up to 8192 rows 54.1 and 51.3: the largest moves lose a little).
   const int pairs = a.n * a.Hkv, waves = (pairs + 147) / 148;
   const int move_here = a.max_moves <= 256 || pairs * 5 >= waves * 148 * 3;
   // About half of the worst case moves, from somewhere to somewhere else: as many bytes as this, of 126 MB.  (67 and 84 MB gain by keeping
