@@ -348,9 +348,9 @@ int mlora_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, do
  * them), rows `*_stride` elements apart (a multiple of 16 bytes), heads packed.  The first rotary_dim features of a head (a
  * multiple of 16) turn in pairs (i, i + rotary_dim / 2) (interleaved = 0) or (2 i, 2 i + 1) (1), the others and v pass through.
  * freq: dev double [rotary_dim / 2], gain: see mlora_rope_frequencies.  q_out dev fp16 [rows][n_q_heads][head_dim]; it may be q
- * itself where q is fp16 and packed.  own_weight, own_position (NULL: not kept): the new rows' entries become 0 and
- * positions[r].  q and q_out NULL: append only.  k, v, own_k, own_v NULL: rotate q only (n_streams * n_nodes rows,
- * suffix_len and status not read).  suffix_len is not changed.  n_nodes has no limit here: with n_streams = 1 and
+ * itself where q is fp16 and packed, and does not overlap it otherwise.  own_weight, own_position (NULL: not kept): the new
+ * rows' entries become 0 and positions[r].  q and q_out NULL: append only.  k, v, own_k, own_v NULL: rotate q only (n_streams *
+ * n_nodes rows, suffix_len and status not read).  suffix_len is not changed.  n_nodes has no limit here: with n_streams = 1 and
  * own_capacity = prefix_len this fills a shared prefix.
  * Errors: ARG, UNSUPPORTED, CAPACITY (n_nodes > own_capacity), CUDA; a stream whose rows do not fit behind suffix_len[stream]
  * appends nothing and sets the device status to MLORA_ERR_CAPACITY. */
@@ -367,8 +367,8 @@ size_t mlora_attention_scored_workspace_bytes(int32_t n_streams, int32_t n_nodes
  * the stream's n_nodes rows and the query heads that share KV head h, of the weight they give row j of the own segment (cached
  * rows and the pass's own); prefix_weight dev fp32 [n_kv_heads][prefix_len] (NULL: not wanted) by the same sum over the rows of
  * all streams.  Entries of rows behind suffix_len + n_nodes are not touched.  tree_parent may be NULL: the pass's rows form a
- * chain.  n_nodes <= 64.  The rows of a pass should be finite: a weight of zero times an infinite or NaN value is NaN.  Results do
- * not depend on the order in which the GPU runs the work.
+ * chain.  n_nodes <= 64.  out does not overlap q.  The rows of a pass should be finite: a weight of zero times an infinite or
+ * NaN value is NaN.  Results do not depend on the order in which the GPU runs the work.
  * Errors: ARG, UNSUPPORTED, CAPACITY (suffix_bound + n_nodes > own_capacity, workspace), CUDA; a malformed parent array or a
  * suffix_len outside 0..suffix_bound sets the device status to MLORA_ERR_ARG. */
 int mlora_attention_scored(const void* q, const void* prefix_k, const void* prefix_v, int32_t prefix_len,

@@ -2014,6 +2014,12 @@ static bool misaligned16(std::initializer_list<const void*> ptrs) {
   return (bits & 15) != 0;
 }
 
+// do byte ranges meet
+static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + nb && y < x + na;
+}
+
 int mlora_rope_append(const void* q, const void* k, const void* v, int32_t in_fp32, int64_t q_stride, int64_t k_stride,
                       int64_t v_stride, const int32_t* positions, const double* freq, float gain, int32_t rotary_dim,
                       int32_t interleaved, int32_t n, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, void* q_out, void* own_k,
@@ -2037,6 +2043,10 @@ int mlora_rope_append(const void* q, const void* k, const void* v, int32_t in_fp
     return fail(MLORA_ERR_ARG, "rope_append: row strides must cover a row and be multiples of 16 bytes");
   if (misaligned16({q, k, v, q_out, own_k, own_v})) return fail(MLORA_ERR_ARG, "rope_append: tensors must be 16-byte aligned");
   if (q && q == q_out && (in_fp32 || q_stride != (int64_t)Hq * hd)) return fail(MLORA_ERR_ARG, "rope_append: in place only for packed fp16 rows");
+  if (q && q != q_out) {
+    const size_t rows = (size_t)n * T, row = (size_t)Hq * hd;
+    if (overlap(q, ((rows - 1) * (size_t)q_stride + row) * (in_fp32 ? 4 : 2), q_out, rows * row * 2)) return fail(MLORA_ERR_ARG, "rope_append: q_out overlaps q");
+  }
   RopeArgs a{};
   a.q = q; a.k = k; a.v = v; a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
   a.positions = positions; a.freq = freq; a.gain = gain; a.in_fp32 = in_fp32 != 0; a.interleaved = interleaved != 0; a.rotary = rotary_dim;
@@ -2083,6 +2093,8 @@ int mlora_attention_scored(const void* q, const void* prefix_k, const void* pref
   float* const ws = (float*)(((uintptr_t)workspace + 15) & ~(uintptr_t)15);
   if (workspace_bytes < (size_t)((unsigned char*)ws - (unsigned char*)workspace) + scored_workspace_floats(a) * sizeof(float))
     return fail(MLORA_ERR_CAPACITY, "attention_scored: workspace too small");
+  const size_t row_bytes = (size_t)n * T * Hq * hd * 2;    // (q is read again when the first rows of out are there)
+  if (overlap(q, row_bytes, out, row_bytes)) return fail(MLORA_ERR_ARG, "attention_scored: out overlaps q");
   if (init_kernels() != MLORA_OK) return MLORA_ERR_CUDA;
   scored_carve(a, ws);
   a.q = (const __half*)q; a.prefix_k = (const __half*)prefix_k; a.prefix_v = (const __half*)prefix_v;

@@ -125,6 +125,19 @@ def test_attention_scored_refuses(mb, code, change):
     assert b"attention_scored" in mb.lib().mlora_last_error(None)
 
 
+@pytest.mark.parametrize("out", [A, A + 2 * 3 * 8 * 64 * 2 - 16, A - 16])
+def test_attention_scored_refuses_out_over_q(mb, out):
+    assert call(mb, "mlora_attention_scored", SCORED, out=out) == ARG
+    assert b"overlaps" in mb.lib().mlora_last_error(None)
+
+
+@pytest.mark.parametrize("change", [dict(q_out=A + 16), dict(q_out=A + 2 * 3 * 512 * 2 - 16), dict(q_out=A - 16), dict(q_stride=1024, q_out=A + 5 * 1024 * 2),
+                                    dict(in_fp32=1, q_out=A + 2 * 3 * 512 * 4 - 16)])
+def test_rope_append_refuses_q_out_over_q(mb, change):
+    assert call(mb, "mlora_rope_append", ROPE, **change) == ARG
+    assert b"overlaps" in mb.lib().mlora_last_error(None)
+
+
 EVICT = dict(own_k=A, own_v=A, own_weight=A, own_position=A, cap=64, suffix_len=A, suffix_bound=40, newest=A, budget=32, recent=4, n=2,
              Hkv=2, hd=64, out_weight=A, out_position=A, out_len=2 * A, out_source=None, workspace=A, workspace_bytes=1 << 30, status=A,
              stream=None)

@@ -381,6 +381,27 @@ def test_evict_without_positions_and_bad_length(mb):
 
 
 # ------------------------------------------------------------------ refusals of the binding, streams, graphs, large offsets
+@pytest.mark.parametrize("T", [1, 16])
+def test_scored_writes_right_behind_its_rows(mb, T):
+    """q and out as the two halves of one buffer; out over q is refused and writes nothing"""
+    rng = np.random.default_rng(31)
+    n, Hq, Hkv, hd, P, cap = 8, 32, 8, 64, 512, 320
+    both = dev(rng.standard_normal((2, n * T, Hq, hd)).astype(np.float16))
+    q, out, apart = both[0], both[1], torch.empty(n * T, Hq, hd, dtype=torch.float16, device="cuda")
+    pk, pv = (dev(rng.standard_normal((Hkv, P, hd)).astype(np.float16)) for _ in range(2))
+    k, v = (dev(rng.standard_normal((n, Hkv, cap, hd)).astype(np.float16)) for _ in range(2))
+    lens, st, bound = i32([30 * s for s in range(n)]), status(), 256
+    w, w2 = torch.zeros(n, Hkv, cap, device="cuda"), torch.zeros(n, Hkv, cap, device="cuda")
+    ws = torch.empty(mb.mlora_attention_scored_workspace_bytes(n, T, Hq, Hkv, hd, P, bound), dtype=torch.uint8, device="cuda")
+    mb.mlora_attention_scored(q, pk, pv, k, v, lens, bound, None, apart, w, None, ws, st)
+    mb.mlora_attention_scored(q, pk, pv, k, v, lens, bound, None, out, w2, None, ws, st)
+    assert torch.equal(out, apart) and torch.equal(w, w2) and int(st.item()) == 0
+    before = q.clone()
+    with pytest.raises(mb.MloraError) as e:
+        mb.mlora_attention_scored(q, pk, pv, k, v, lens, bound, None, q, w2, None, ws, st)
+    assert e.value.code == -1 and torch.equal(q, before) and torch.equal(w, w2)
+
+
 def test_binding_refuses_wrong_tensors(mb):
     n, T, Hq, Hkv, hd, cap = 2, 1, 4, 2, 64, 32
     f = lambda *s, t=torch.float16: torch.zeros(*s, dtype=t, device="cuda")  # noqa: E731
