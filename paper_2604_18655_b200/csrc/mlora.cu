@@ -2127,7 +2127,11 @@ int mlora_kv_evict(void* own_k, void* own_v, const float* own_weight, const int3
   if (hd != 64 && hd != 128) return fail(MLORA_ERR_UNSUPPORTED, "kv_evict: head_dim must be 64 or 128");
   if (suffix_bound > own_capacity) return fail(MLORA_ERR_CAPACITY, "kv_evict: suffix_bound exceeds own_capacity");
   if (misaligned16({own_k, own_v})) return fail(MLORA_ERR_ARG, "kv_evict: K and V must be 16-byte aligned");
-  if (suffix_len == out_len) return fail(MLORA_ERR_ARG, "kv_evict: out_len must not be suffix_len");
+  const size_t lens = (size_t)n * sizeof(int32_t), entries = (size_t)n * Hkv * own_capacity * 4;
+  if (overlap(suffix_len, lens, out_len, lens) || (recent > 0 && overlap(newest, lens, out_len, lens))) return fail(MLORA_ERR_ARG, "kv_evict: out_len overlaps suffix_len or newest");
+  if ((out_weight != own_weight && overlap(out_weight, entries, own_weight, entries)) ||
+      (own_position && out_position != own_position && overlap(out_position, entries, own_position, entries)))
+    return fail(MLORA_ERR_ARG, "kv_evict: out_weight and out_position are own_weight and own_position or do not overlap them");
   EvictArgs a{};
   a.own_k = (__half*)own_k; a.own_v = (__half*)own_v; a.weight = own_weight; a.position = own_position;
   a.out_weight = out_weight; a.out_position = out_position; a.suffix_len = suffix_len; a.newest = newest; a.out_len = out_len;

@@ -155,6 +155,13 @@ def test_kv_evict_refuses(mb, code, change):
     assert b"kv_evict" in mb.lib().mlora_last_error(None)
 
 
+@pytest.mark.parametrize("change", [dict(out_len=A + 4), dict(out_len=A - 4), dict(suffix_len=4 * A, out_len=A), dict(suffix_len=4 * A, out_len=A + 4),
+                                    dict(out_weight=A + 256), dict(out_weight=A - 4), dict(out_position=A + 2 * 2 * 64 * 4 - 4)])
+def test_kv_evict_refuses_overlaps(mb, change):
+    assert call(mb, "mlora_kv_evict", EVICT, **change) == ARG
+    assert b"overlap" in mb.lib().mlora_last_error(None)
+
+
 # ------------------------------------------------------------------ workspaces
 @pytest.mark.parametrize("n,T,Hq,Hkv,hd,P", [(1, 1, 32, 8, 64, 512), (8, 1, 24, 8, 128, 0), (3, 7, 8, 2, 64, 100), (8, 32, 24, 8, 128, 2048)])
 def test_scored_workspace_covers_every_smaller_bound(mb, n, T, Hq, Hkv, hd, P):
