@@ -348,10 +348,11 @@ int mlora_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, do
  * them), rows `*_stride` elements apart (a multiple of 16 bytes), heads packed.  The first rotary_dim features of a head (a
  * multiple of 16) turn in pairs (i, i + rotary_dim / 2) (interleaved = 0) or (2 i, 2 i + 1) (1), the others and v pass through.
  * freq: dev double [rotary_dim / 2], gain: see mlora_rope_frequencies.  q_out dev fp16 [rows][n_q_heads][head_dim]; it may be q
- * itself where q is fp16 and packed, and does not overlap it otherwise.  own_weight, own_position (NULL: not kept): the new
- * rows' entries become 0 and positions[r].  q and q_out NULL: append only.  k, v, own_k, own_v NULL: rotate q only (n_streams *
- * n_nodes rows, suffix_len and status not read).  suffix_len is not changed.  n_nodes has no limit here: with n_streams = 1 and
- * own_capacity = prefix_len this fills a shared prefix.
+ * itself where q is fp16 and packed.  Otherwise nothing that is written overlaps what is read, or anything else written (rows of
+ * k and v are not taken from the segments themselves).  own_weight, own_position (NULL: not kept): the new rows' entries become 0
+ * and positions[r].  q and q_out NULL: append only.  k, v, own_k, own_v NULL: rotate q only (n_streams * n_nodes rows, suffix_len
+ * and status not read).  suffix_len is not changed.  n_nodes has no limit here: with n_streams = 1 and own_capacity = prefix_len
+ * this fills a shared prefix.
  * Errors: ARG, UNSUPPORTED, CAPACITY (n_nodes > own_capacity), CUDA; a stream whose rows do not fit behind suffix_len[stream]
  * appends nothing and sets the device status to MLORA_ERR_CAPACITY. */
 int mlora_rope_append(const void* q, const void* k, const void* v, int32_t in_fp32, int64_t q_stride, int64_t k_stride,

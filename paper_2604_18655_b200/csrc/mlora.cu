@@ -2017,7 +2017,20 @@ static bool misaligned16(std::initializer_list<const void*> ptrs) {
 // do byte ranges meet
 static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x < y + nb && y < x + na;
+  return na != 0 && nb != 0 && x < y + nb && y < x + na;
+}
+
+struct Span { const void* at; size_t bytes; };             // null: not given
+// does anything written meet anything read, or anything else written
+static bool outputs_meet(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  for (const Span* o = outs.begin(); o != outs.end(); ++o) {
+    if (o->at == nullptr) continue;
+    for (const Span& i : ins)
+      if (i.at != nullptr && overlap(o->at, o->bytes, i.at, i.bytes)) return true;
+    for (const Span* x = outs.begin(); x != o; ++x)
+      if (x->at != nullptr && overlap(o->at, o->bytes, x->at, x->bytes)) return true;
+  }
+  return false;
 }
 
 int mlora_rope_append(const void* q, const void* k, const void* v, int32_t in_fp32, int64_t q_stride, int64_t k_stride,
@@ -2043,10 +2056,15 @@ int mlora_rope_append(const void* q, const void* k, const void* v, int32_t in_fp
     return fail(MLORA_ERR_ARG, "rope_append: row strides must cover a row and be multiples of 16 bytes");
   if (misaligned16({q, k, v, q_out, own_k, own_v})) return fail(MLORA_ERR_ARG, "rope_append: tensors must be 16-byte aligned");
   if (q && q == q_out && (in_fp32 || q_stride != (int64_t)Hq * hd)) return fail(MLORA_ERR_ARG, "rope_append: in place only for packed fp16 rows");
-  if (q && q != q_out) {
-    const size_t rows = (size_t)n * T, row = (size_t)Hq * hd;
-    if (overlap(q, ((rows - 1) * (size_t)q_stride + row) * (in_fp32 ? 4 : 2), q_out, rows * row * 2)) return fail(MLORA_ERR_ARG, "rope_append: q_out overlaps q");
-  }
+  // (another CTA may still have to read what this one would overwrite)
+  const size_t rows = (size_t)n * T, q_row = (size_t)Hq * hd, kv_row = (size_t)Hkv * hd, size = in_fp32 ? 4 : 2, q_out_bytes = rows * q_row * 2;
+  const Span q_in{q == q_out ? nullptr : q, ((rows - 1) * (size_t)q_stride + q_row) * size};
+  if (q_in.at && overlap(q_in.at, q_in.bytes, q_out, q_out_bytes)) return fail(MLORA_ERR_ARG, "rope_append: q_out overlaps q");
+  const size_t entries = (size_t)n * Hkv * own_capacity * 4, segments = entries / 2 * hd;
+  if (outputs_meet({{q_out, q_out_bytes}, {own_k, segments}, {own_v, segments}, {own_weight, entries}, {own_position, entries}},
+                   {q_in, {k, ((rows - 1) * (size_t)k_stride + kv_row) * size}, {v, ((rows - 1) * (size_t)v_stride + kv_row) * size},
+                    {positions, rows * sizeof(int32_t)}, {freq, rotary_dim / 2 * sizeof(double)}, {app ? suffix_len : nullptr, n * sizeof(int32_t)}}))
+    return fail(MLORA_ERR_ARG, "rope_append: what is written overlaps what is read, or each other");
   RopeArgs a{};
   a.q = q; a.k = k; a.v = v; a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
   a.positions = positions; a.freq = freq; a.gain = gain; a.in_fp32 = in_fp32 != 0; a.interleaved = interleaved != 0; a.rotary = rotary_dim;

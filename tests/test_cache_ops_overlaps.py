@@ -1,0 +1,44 @@
+"""Calls around a bounded KV cache whose tensors lie over each other: refused on the host, each by the check that is meant.  The base
+arguments of every call are apart, so that one change is one fault.  No GPU."""
+import pytest
+
+ARG = -1
+STEP = 1 << 32                                     # stands for aligned addresses that are far apart; a refused call reads none
+A = [STEP * (i + 1) for i in range(16)]
+
+
+@pytest.fixture(scope="module")
+def mb():
+    from paper_2604_18655_b200 import binding, build
+    build.build()
+    binding.lib()
+    return binding
+
+
+def refused(mb, name, good, change):
+    assert set(change) <= set(good)
+    assert getattr(mb.lib(), name)(*{**good, **change}.values()) == ARG
+    return mb.lib().mlora_last_error(None).decode()
+
+
+# two streams of three rows, 8 query heads and 2 KV heads of 64, segments of 16 rows
+ROPE = dict(q=A[0], k=A[1], v=A[2], in_fp32=0, q_stride=512, k_stride=128, v_stride=128, positions=A[3], freq=A[4], gain=1.0, rotary_dim=64,
+            interleaved=0, n=2, T=3, Hq=8, Hkv=2, hd=64, q_out=A[5], own_k=A[6], own_v=A[7], cap=16, suffix_len=A[8], own_weight=A[9],
+            own_position=A[10], status=A[11], stream=None)
+SEG, ROWS_KV, ROWS_Q = 2 * 2 * 16 * 64 * 2, 6 * 128 * 2, 6 * 512 * 2
+
+
+@pytest.mark.parametrize("change", [
+    dict(own_k=A[1]), dict(own_v=A[2]), dict(own_k=A[2]), dict(own_v=A[1] + ROWS_KV - 16), dict(own_k=A[1] - SEG + 16),
+    dict(own_v=A[0]), dict(own_k=A[0] + ROWS_Q - 16), dict(own_v=A[6]), dict(own_v=A[6] + SEG - 16),
+    dict(q_out=A[1]), dict(q_out=A[2] + ROWS_KV - 16), dict(q_out=A[1] - ROWS_Q + 16), dict(q_out=A[6]), dict(q_out=A[7] + SEG - 16),
+    dict(own_weight=A[3]), dict(own_position=A[3] + 5 * 4), dict(own_weight=A[4] + 31 * 8), dict(own_position=A[8] + 4), dict(own_position=A[9]),
+    dict(own_k=A[8]), dict(own_weight=A[6]), dict(own_position=A[2]),
+    # strided rows reach as far as their last one; fp32 rows twice as far
+    dict(k_stride=384, own_k=A[1] + 5 * 384 * 2 + 128 * 2 - 16), dict(in_fp32=1, own_v=A[2] + 2 * ROWS_KV - 16),
+    # append only, rotate only
+    dict(q=None, q_out=None, own_k=A[1]), dict(k=None, v=None, own_k=None, own_v=None, own_weight=None, own_position=None, q_out=A[3]),
+    # a segment's own rows as the rows to append: a later row's source is an earlier one's place
+    dict(q=None, q_out=None, Hkv=1, k_stride=64, k=A[6] + 64 * 2)])
+def test_rope_append_refuses_outputs_over_what_it_reads(mb, change):
+    assert "overlaps" in refused(mb, "mlora_rope_append", ROPE, change)
