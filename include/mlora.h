@@ -368,8 +368,9 @@ size_t mlora_attention_scored_workspace_bytes(int32_t n_streams, int32_t n_nodes
  * the stream's n_nodes rows and the query heads that share KV head h, of the weight they give row j of the own segment (cached
  * rows and the pass's own); prefix_weight dev fp32 [n_kv_heads][prefix_len] (NULL: not wanted) by the same sum over the rows of
  * all streams.  Entries of rows behind suffix_len + n_nodes are not touched.  tree_parent may be NULL: the pass's rows form a
- * chain.  n_nodes <= 64.  out does not overlap q.  The rows of a pass should be finite: a weight of zero times an infinite or
- * NaN value is NaN.  Results do not depend on the order in which the GPU runs the work.
+ * chain.  n_nodes <= 64.  out, own_weight, prefix_weight and the workspace overlap neither each other nor what is read.  The rows
+ * of a pass should be finite: a weight of zero times an infinite or NaN value is NaN.  Results do not depend on the order in which
+ * the GPU runs the work.
  * Errors: ARG, UNSUPPORTED, CAPACITY (suffix_bound + n_nodes > own_capacity, workspace), CUDA; a malformed parent array or a
  * suffix_len outside 0..suffix_bound sets the device status to MLORA_ERR_ARG. */
 int mlora_attention_scored(const void* q, const void* prefix_k, const void* prefix_v, int32_t prefix_len,

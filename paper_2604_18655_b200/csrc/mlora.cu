@@ -2109,10 +2109,16 @@ int mlora_attention_scored(const void* q, const void* prefix_k, const void* pref
   if (misaligned16({q, prefix_k, prefix_v, own_k, own_v, out})) return fail(MLORA_ERR_ARG, "attention_scored: q, K, V and out must be 16-byte aligned");
   ScoredArgs a = scored_fill(n, T, Hq, Hkv, hd, P, suffix_bound);
   float* const ws = (float*)(((uintptr_t)workspace + 15) & ~(uintptr_t)15);
-  if (workspace_bytes < (size_t)((unsigned char*)ws - (unsigned char*)workspace) + scored_workspace_floats(a) * sizeof(float))
-    return fail(MLORA_ERR_CAPACITY, "attention_scored: workspace too small");
+  const size_t used = (size_t)((unsigned char*)ws - (unsigned char*)workspace) + scored_workspace_floats(a) * sizeof(float);
+  if (workspace_bytes < used) return fail(MLORA_ERR_CAPACITY, "attention_scored: workspace too small");
   const size_t row_bytes = (size_t)n * T * Hq * hd * 2;    // (q is read again when the first rows of out are there)
   if (overlap(q, row_bytes, out, row_bytes)) return fail(MLORA_ERR_ARG, "attention_scored: out overlaps q");
+  // (keys are read again too, and old totals while partial results are written)
+  const size_t prefix = (size_t)Hkv * P, entries = (size_t)n * Hkv * own_capacity;
+  if (outputs_meet({{out, row_bytes}, {own_weight, entries * 4}, {P > 0 ? prefix_weight : nullptr, prefix * 4}, {workspace, used}},
+                   {{q, row_bytes}, {P > 0 ? prefix_k : nullptr, prefix * hd * 2}, {P > 0 ? prefix_v : nullptr, prefix * hd * 2}, {own_k, entries * hd * 2},
+                    {own_v, entries * hd * 2}, {suffix_len, n * sizeof(int32_t)}, {tree_parent, (size_t)n * T * sizeof(int32_t)}}))
+    return fail(MLORA_ERR_ARG, "attention_scored: what is written overlaps what is read, or each other");
   if (init_kernels() != MLORA_OK) return MLORA_ERR_CUDA;
   scored_carve(a, ws);
   a.q = (const __half*)q; a.prefix_k = (const __half*)prefix_k; a.prefix_v = (const __half*)prefix_v;

@@ -42,3 +42,19 @@ SEG, ROWS_KV, ROWS_Q = 2 * 2 * 16 * 64 * 2, 6 * 128 * 2, 6 * 512 * 2
     dict(q=None, q_out=None, Hkv=1, k_stride=64, k=A[6] + 64 * 2)])
 def test_rope_append_refuses_outputs_over_what_it_reads(mb, change):
     assert "overlaps" in refused(mb, "mlora_rope_append", ROPE, change)
+
+
+# two streams of three rows, 8 query heads and 2 KV heads of 64 behind 32 keys, segments of 64 rows
+SCORED = dict(q=A[0], prefix_k=A[1], prefix_v=A[2], P=32, own_k=A[3], own_v=A[4], cap=64, suffix_len=A[5], suffix_bound=40, tree_parent=A[6], n=2, T=3,
+              Hq=8, Hkv=2, hd=64, out=A[7], own_weight=A[8], prefix_weight=A[9], workspace=A[10], workspace_bytes=STEP, status=A[11], stream=None)
+PREFIX, OWN, TOTALS = 2 * 32 * 64 * 2, 2 * 2 * 64 * 64 * 2, 2 * 2 * 64 * 4
+
+
+@pytest.mark.parametrize("change", [
+    dict(out=A[0]), dict(out=A[1]), dict(out=A[2] + PREFIX - 16), dict(out=A[3] - ROWS_Q + 16), dict(out=A[4] + OWN - 16), dict(own_weight=A[1]),
+    dict(own_weight=A[5] + 4), dict(own_weight=A[6] + 5 * 4), dict(own_weight=A[7] + ROWS_Q - 4), dict(prefix_weight=A[8] + TOTALS - 4),
+    dict(prefix_weight=A[4]), dict(prefix_weight=A[7]), dict(prefix_weight=A[8] - 2 * 32 * 4 + 4), dict(own_weight=A[0]),
+    dict(workspace=A[0]), dict(workspace=A[3] + OWN - 16), dict(workspace=A[8]), dict(workspace=A[9] + 2 * 32 * 4 - 4), dict(workspace=A[7]), dict(workspace=A[6] - 64),
+    dict(P=0, prefix_k=None, prefix_v=None, prefix_weight=None, out=A[3])])
+def test_attention_scored_refuses_outputs_over_what_it_reads(mb, change):
+    assert "overlaps" in refused(mb, "mlora_attention_scored", SCORED, change)

@@ -38,3 +38,27 @@ def test_rope_append_between_tensors_that_touch(mb):  # noqa: F811
     mb.mlora_rope_append(*apart[:5], *apart[5:8], lens, st, own_weight=apart[8], own_position=apart[9])
     assert int(st.item()) == 0
     assert all(torch.equal(a, b) for a, b in zip((q, k, v, pos, freq, qo, ok, ov, w, p), apart))
+
+
+@pytest.mark.parametrize("T", [1, 20])
+def test_scored_between_tensors_that_touch(mb, T):  # noqa: F811
+    """As above, the workspace among them, of the queried size to the byte; and no prefix totals where there is no prefix"""
+    n, Hq, Hkv, hd, cap, P, bound = 2, 8, 2, 64, 64, 32, 40
+    f16, f32, i4 = torch.float16, torch.float32, torch.int32
+    need = mb.mlora_attention_scored_workspace_bytes(n, T, Hq, Hkv, hd, P, bound)
+    ws, q, pk, out, pv, ok, w, ov, pw, ws2 = arena([
+        (((need + 15) // 16 * 16,), torch.uint8), ((n * T, Hq, hd), f16), ((Hkv, P, hd), f16), ((n * T, Hq, hd), f16), ((Hkv, P, hd), f16),
+        ((n, Hkv, cap, hd), f16), ((n, Hkv, cap), f32), ((n, Hkv, cap, hd), f16), ((Hkv, P), f32), ((4096,), torch.uint8)])
+    g = torch.Generator(device="cuda").manual_seed(0)
+    for t in (q, pk, pv, ok, ov, w, pw):
+        t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+    ws.fill_(255), ws2.fill_(7)
+    lens, st = i32([40, 3]), status()
+    par = i32([[-1] + [i // 2 for i in range(T - 1)]] * n)
+    apart = [t.clone() for t in (q, pk, pv, ok, ov, out, w, pw)]
+    mb.mlora_attention_scored(q, pk, pv, ok, ov, lens, bound, par, out, w, pw, ws[:need], st)
+    mb.mlora_attention_scored(*apart[:5], lens, bound, par, *apart[5:], torch.empty(need, dtype=torch.uint8, device="cuda"), st)
+    assert int(st.item()) == 0 and bool((ws2 == 7).all())
+    assert all(torch.equal(a, b) for a, b in zip((q, pk, pv, ok, ov, out, w, pw), apart))
+    mb.mlora_attention_scored(q, None, None, ok, ov, lens, bound, par, out, w, torch.empty(Hkv, 0, device="cuda"), ws[:need], st)
+    assert int(st.item()) == 0
