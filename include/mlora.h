@@ -386,9 +386,9 @@ size_t mlora_kv_evict_workspace_bytes(int32_t n_streams, int32_t n_kv_heads, int
  * [n_streams]), then falling own_weight (NaN lowest, -0 equals +0), then rising index.  Rows that stay and lie below index
  * `budget` stay where they are; the others that stay move, in rising order, to the places of the dropped rows, in rising
  * order.  Their own_weight and own_position go with them: entries 0 .. out_len[s] - 1 of out_weight and out_position are
- * written for all rows that are left.  out_weight may be own_weight and out_position own_position, else they do not overlap;
- * own_position and out_position may both be NULL where recent is 0.  out_len dev int32 [n_streams] = min(suffix_len, budget),
- * overlaps neither suffix_len nor newest.
+ * written for all rows that are left.  out_weight may be own_weight and out_position own_position; otherwise nothing that is
+ * written (own_k, own_v and the workspace too) overlaps what is read or anything else written.  own_position and out_position may
+ * both be NULL where recent is 0.  out_len dev int32 [n_streams] = min(suffix_len, budget).
  * out_source dev int32 [n_streams][n_kv_heads][budget] or NULL: the index that each row had before.
  * Rows and entries from index out_len[s] on are left as they were.
  * Errors: ARG (recent > budget, ...), UNSUPPORTED, CAPACITY (suffix_bound > own_capacity, workspace), CUDA; a suffix_len

@@ -2163,8 +2163,14 @@ int mlora_kv_evict(void* own_k, void* own_v, const float* own_weight, const int3
   a.recent = recent; a.max_moves = evict_max_moves(suffix_bound, budget); a.status = status;
   unsigned char* const ws = (unsigned char*)(((uintptr_t)workspace + 15) & ~(uintptr_t)15);
   const size_t counts = ((size_t)n * Hkv * sizeof(int32_t) + 15) / 16 * 16;
-  if (workspace_bytes < (size_t)(ws - (unsigned char*)workspace) + counts + (size_t)n * Hkv * a.max_moves * sizeof(int2))
-    return fail(MLORA_ERR_CAPACITY, "kv_evict: workspace too small");
+  const size_t used = (size_t)(ws - (unsigned char*)workspace) + counts + (size_t)n * Hkv * a.max_moves * sizeof(int2);
+  if (workspace_bytes < used) return fail(MLORA_ERR_CAPACITY, "kv_evict: workspace too small");
+  const size_t segments = entries / 2 * hd;
+  if (outputs_meet({{own_k, segments}, {own_v, segments}, {out_weight, entries}, {out_position, entries}, {out_len, lens},
+                    {out_source, (size_t)n * Hkv * budget * sizeof(int32_t)}, {workspace, used}},
+                   {{out_weight == own_weight ? nullptr : own_weight, entries}, {out_position == own_position ? nullptr : own_position, entries},
+                    {suffix_len, lens}, {recent > 0 ? newest : nullptr, lens}}))
+    return fail(MLORA_ERR_ARG, "kv_evict: what is written overlaps what is read, or each other");
   a.counts = (int32_t*)ws; a.moves = (int2*)(ws + counts);
   CK(launch_kv_evict(a, (cudaStream_t)cuda_stream));
   return MLORA_OK;

@@ -58,3 +58,21 @@ PREFIX, OWN, TOTALS = 2 * 32 * 64 * 2, 2 * 2 * 64 * 64 * 2, 2 * 2 * 64 * 4
     dict(P=0, prefix_k=None, prefix_v=None, prefix_weight=None, out=A[3])])
 def test_attention_scored_refuses_outputs_over_what_it_reads(mb, change):
     assert "overlaps" in refused(mb, "mlora_attention_scored", SCORED, change)
+
+
+# two streams of 2 KV heads of 64, segments of 64 rows cut to 32
+EVICT = dict(own_k=A[0], own_v=A[1], own_weight=A[2], own_position=A[3], cap=64, suffix_len=A[4], suffix_bound=40, newest=A[5], budget=32, recent=4, n=2,
+             Hkv=2, hd=64, out_weight=A[6], out_position=A[7], out_len=A[8], out_source=A[9], workspace=A[10], workspace_bytes=STEP, status=A[11], stream=None)
+SOURCE = 2 * 2 * 32 * 4
+IN_PLACE = dict(out_weight=A[2], out_position=A[3])
+
+
+@pytest.mark.parametrize("change", [
+    dict(own_v=A[0]), dict(own_v=A[0] + OWN - 16), dict(own_k=A[2]), dict(own_weight=A[1] + OWN - 4), dict(out_weight=A[3]), dict(out_position=A[2] + TOTALS - 4),
+    dict(out_weight=A[7]), dict(out_weight=A[0]), dict(out_position=A[1] + OWN - 4), dict(out_len=A[2]), dict(out_len=A[6] + TOTALS - 4), dict(out_len=A[4] + 4),
+    dict(out_len=A[5]), dict(out_weight=A[4]), dict(out_position=A[5] - TOTALS + 4), dict(out_source=A[2]), dict(out_source=A[3] + TOTALS - 4), dict(out_source=A[7]),
+    dict(out_source=A[8]), dict(out_source=A[4] - SOURCE + 4), dict(workspace=A[0]), dict(workspace=A[2]), dict(workspace=A[7] + TOTALS - 16), dict(workspace=A[4]),
+    dict(workspace=A[9] + SOURCE - 16), dict(workspace=A[8]), dict(out_weight=A[2] + 4), dict(out_position=A[3] - 4),
+    {**IN_PLACE, "out_len": A[2]}, {**IN_PLACE, "out_source": A[3]}, {**IN_PLACE, "own_v": A[3]}, dict(out_weight=A[3], out_position=A[2])])
+def test_kv_evict_refuses_outputs_over_what_it_reads(mb, change):
+    assert "overlap" in refused(mb, "mlora_kv_evict", EVICT, change)

@@ -62,3 +62,28 @@ def test_scored_between_tensors_that_touch(mb, T):  # noqa: F811
     assert all(torch.equal(a, b) for a, b in zip((q, pk, pv, ok, ov, out, w, pw), apart))
     mb.mlora_attention_scored(q, None, None, ok, ov, lens, bound, par, out, w, torch.empty(Hkv, 0, device="cuda"), ws[:need], st)
     assert int(st.item()) == 0
+
+
+@pytest.mark.parametrize("recent,in_place", [(0, False), (4, False), (4, True)])
+def test_evict_between_tensors_that_touch(mb, recent, in_place):  # noqa: F811
+    """As above; newest may be out_len where no row is kept for being new: it is not read then"""
+    n, Hkv, hd, cap, B = 4, 2, 64, 64, 32
+    f16, f32, i4 = torch.float16, torch.float32, torch.int32
+    need = mb.mlora_kv_evict_workspace_bytes(n, Hkv, cap, B)
+    lens, k, w, p, v, ow, op, ol, src, newest, ws = arena([
+        ((n,), i4), ((n, Hkv, cap, hd), f16), ((n, Hkv, cap), f32), ((n, Hkv, cap), i4), ((n, Hkv, cap, hd), f16), ((n, Hkv, cap), f32), ((n, Hkv, cap), i4),
+        ((n,), i4), ((n, Hkv, B), i4), ((n,), i4), (((need + 15) // 16 * 16,), torch.uint8)])
+    g = torch.Generator(device="cuda").manual_seed(0)
+    for t in (k, v, w):
+        t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+    p.copy_(torch.arange(cap, device="cuda"))
+    lens.copy_(i32([64, 50, 33, 7])), newest.copy_(lens - 1)
+    st = status()
+    apart = [t.clone() for t in (k, v, w, p, lens, newest, ow, op, ol, src)]
+    if in_place:
+        ow, op = w, p
+        apart[6:8] = apart[2:4]
+    mb.mlora_kv_evict(k, v, w, p, lens, cap, newest if recent else ol, B, recent, ow, op, ol, ws[:need], st, out_source=src)
+    mb.mlora_kv_evict(*apart[:5], cap, apart[5], B, recent, *apart[6:9], torch.empty(need, dtype=torch.uint8, device="cuda"), st, out_source=apart[9])
+    assert int(st.item()) == 0 and ol.tolist() == [32, 32, 32, 7]
+    assert all(torch.equal(a, b) for a, b in zip((k, v, w, p, lens, newest, ow, op, ol, src), apart))
