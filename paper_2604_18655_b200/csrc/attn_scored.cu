@@ -82,6 +82,8 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
     const size_t seg = ((size_t)s * p.Hkv + kh) * p.cap * HD;
     kb = p.own_k + seg; vb = p.own_v + seg;
     sc = p.sc_own; ld = p.ld_own;
+    // (a single row has no mask to make; what its parent says is checked all the same)
+    if (p.T == 1 && p.parent != nullptr && k1 > S && tid == 0 && p.parent[s] != -1) atomicCAS(p.status, 0, MLORA_ERR_ARG);
     if (p.T > 1 && k1 > S && tid < 16) {                   // ancestor-or-self masks of the tile's nodes
       unsigned long long mask = 0ull;
       if (v0 + tid < v1) {

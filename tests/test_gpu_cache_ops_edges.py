@@ -87,3 +87,25 @@ def test_evict_between_tensors_that_touch(mb, recent, in_place):  # noqa: F811
     mb.mlora_kv_evict(*apart[:5], cap, apart[5], B, recent, *apart[6:9], torch.empty(need, dtype=torch.uint8, device="cuda"), st, out_source=apart[9])
     assert int(st.item()) == 0 and ol.tolist() == [32, 32, 32, 7]
     assert all(torch.equal(a, b) for a, b in zip((k, v, w, p, lens, newest, ow, op, ol, src), apart))
+
+
+# n, T, Hq, Hkv, hd, P: by the kernels for few rows, by those on tensor memory, one row a stream by both
+@pytest.mark.parametrize("n,T,Hq,Hkv,hd,P", [(2, 1, 8, 2, 64, 16), (2, 1, 8, 8, 128, 0), (2, 3, 4, 2, 64, 16), (2, 40, 32, 8, 64, 500), (2, 64, 24, 8, 128, 600),
+                                            (32, 1, 32, 8, 64, 6001)])
+def test_scored_reports_every_malformed_parent(mb, n, T, Hq, Hkv, hd, P):  # noqa: F811
+    """One wrong entry of the last stream, whatever kernels the sizes pick: a root that has a parent, a node whose parent is itself, a later
+    node, none or out of range"""
+    z = lambda *s: torch.zeros(*s, dtype=torch.float16, device="cuda")  # noqa: E731
+    bound, cap = 30, 30 + T
+    q, out, pk, pv, k, v = z(n * T, Hq, hd), z(n * T, Hq, hd), z(Hkv, P, hd), z(Hkv, P, hd), z(n, Hkv, cap, hd), z(n, Hkv, cap, hd)
+    w = torch.zeros(n, Hkv, cap, device="cuda")
+    ws = torch.empty(mb.mlora_attention_scored_workspace_bytes(n, T, Hq, Hkv, hd, P, bound), dtype=torch.uint8, device="cuda")
+    good = [[-1] + [(i - 1) // 2 for i in range(1, T)] for _ in range(n)]
+    wrong = [(0, x) for x in (0, 7, -2, -2**31)] + ([(T - 1, x) for x in (T - 1, T, -1, 2**31 - 1)] + [(1, 1)] if T > 1 else [])
+    for lens in ([0] * n, [bound] * n):
+        for node, value in [(0, -1)] + wrong:
+            par = [list(r) for r in good]
+            par[-1][node] = value
+            st = status()
+            mb.mlora_attention_scored(q, pk if P else None, pv if P else None, k, v, i32(lens), bound, i32(par), out, w, None, ws, st)
+            assert int(st.item()) == (0 if (node, value) == (0, -1) else -1), (lens[0], node, value)
