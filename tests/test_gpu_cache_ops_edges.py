@@ -109,3 +109,44 @@ def test_scored_reports_every_malformed_parent(mb, n, T, Hq, Hkv, hd, P):  # noq
             st = status()
             mb.mlora_attention_scored(q, pk if P else None, pv if P else None, k, v, i32(lens), bound, i32(par), out, w, None, ws, st)
             assert int(st.item()) == (0 if (node, value) == (0, -1) else -1), (lens[0], node, value)
+
+
+def test_readme_example_runs(mb):  # noqa: F811
+    """The example that README gives, as it stands there: what is ahead of the projection once, the rest every step, until the streams are at their budget"""
+    import os
+
+    import gen
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")) as f:
+        text = f.read()
+    blocks = [b.split("```")[0] for b in text.split("```python\n")[1:]]
+    blocks = [b for b in blocks if "mlora_kv_evict" in b]
+    assert len(blocks) == 1
+    once, step = blocks[0].split("mb.mlora_linear(", 1)
+    step = "mb.mlora_linear(" + step
+    n, Hq, Hkv, head_dim, P, budget, recent, K, rank = 2, 8, 2, 64, 40, 16, 4, 256, 8
+    cap, nq, nkv = budget + 1, Hq * head_dim, Hkv * head_dim
+    rng = np.random.default_rng(0)
+    qb, sc = gen.quantize_int4(rng.standard_normal((K, nq + 2 * nkv)).astype(np.float32) * 0.1, 64)
+    r16 = lambda *s: dev(rng.standard_normal(s).astype(np.float16))  # noqa: E731
+    low = [r16(rank, K), r16(rank, nq + 2 * nkv)]
+    e = dict(torch=torch, mb=mb, head_dim=head_dim, nq=nq, nkv=nkv, budget=budget, recent=recent, rank=rank, status=status(),
+             w_qkv=mb.mlora_weight_create(dev(qb), dev(sc), K, nq + 2 * nkv, 64), x=r16(n, K), qkv=torch.empty(n, nq + 2 * nkv, device="cuda"),
+             adapters=i32([0] * n), A=torch.tensor([low[0].data_ptr()], dtype=torch.int64, device="cuda"),
+             B=torch.tensor([low[1].data_ptr()], dtype=torch.int64, device="cuda"), scale=torch.ones(1, device="cuda"),
+             pos=i32([P] * n), q=torch.empty(n, Hq, head_dim, dtype=torch.float16, device="cuda"), own_k=r16(n, Hkv, cap, head_dim),
+             own_v=r16(n, Hkv, cap, head_dim), lens=i32([0] * n), lens_new=i32([0] * n), weight=torch.zeros(n, Hkv, cap, device="cuda"),
+             position=torch.zeros(n, Hkv, cap, dtype=torch.int32, device="cuda"), prefix_k=r16(Hkv, P, head_dim), prefix_v=r16(Hkv, P, head_dim),
+             out=torch.empty(n, Hq, head_dim, dtype=torch.float16, device="cuda"))
+    e["linear_ws"] = torch.zeros(mb.mlora_linear_workspace_bytes(e["w_qkv"], n, rank), dtype=torch.uint8, device="cuda")
+    e["attn_ws"] = torch.empty(mb.mlora_attention_scored_workspace_bytes(n, 1, Hq, Hkv, head_dim, P, budget), dtype=torch.uint8, device="cuda")
+    e["evict_ws"] = torch.empty(mb.mlora_kv_evict_workspace_bytes(n, Hkv, budget + 1, budget), dtype=torch.uint8, device="cuda")
+    exec(once, e)
+    for i in range(budget + 5):
+        e["x"].copy_(r16(n, K))
+        exec(step, e)
+    torch.cuda.synchronize()
+    mb.mlora_weight_destroy(e["w_qkv"])
+    assert int(e["status"].item()) == 0 and e["lens"].tolist() == [budget] * n and e["pos"].tolist() == [P + budget + 5] * n
+    newest = sorted(range(P + budget + 5))[-recent:]
+    for row in e["position"][:, :, :budget].reshape(-1, budget).tolist():
+        assert len(set(row)) == budget and set(newest) <= set(row)
