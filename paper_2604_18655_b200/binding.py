@@ -404,7 +404,7 @@ def mlora_rope_append(q, k, v, positions, freq, q_out, own_k, own_v, suffix_len,
                       own_weight=None, own_position=None):
     """q, k, v: fp16 or fp32 rows [rows][heads * head_dim] or [rows][heads][head_dim], any row stride; positions int32 [rows]; freq
     float64 [rotary_dim / 2]; q_out fp16 [rows][Hq][hd]; own_k, own_v fp16 [n][Hkv][capacity][hd]; suffix_len int32 [n].  q and q_out,
-    or k, v, own_k and own_v, may be None.  Tensors of another type, shape, packing or device than the current one are refused."""
+    or k, v, own_k and own_v, may be None (without those, suffix_len and status are not looked at).  Tensors of another type, shape, packing or device than the current one are refused."""
     r = (_native or _marshal()).rope_append(q, k, v, positions, freq, q_out, own_k, own_v, suffix_len, status, gain, interleaved,
                                             own_weight, own_position)
     if r is not None:

@@ -146,8 +146,8 @@ PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                   (float)number(a[10], "gain"), size32(2 * freq.numel(), "freq"), interleaved, size32(n, "streams"), size32(rows / n, "rows"),
                   size32(Hq, "heads"), size32(Hkv, "heads"), size32(hd, "head_dim"), packed(a[5], F16, {rows, Hq, hd}, dev, "q_out"),
                   packed(a[6], F16, {n, Hkv, cap, hd}, dev, "own_k"), packed(a[7], F16, {n, Hkv, cap, hd}, dev, "own_v"), size32(cap, "own_capacity"),
-                  (const int32_t*)packed(a[8], I32, {n}, dev, "suffix_len"), (float*)packed(a[12], F32, {n, Hkv, cap}, dev, "own_weight"),
-                  (int32_t*)packed(a[13], I32, {n, Hkv, cap}, dev, "own_position"), (int32_t*)packed(a[9], I32, {1}, dev, "status"),
+                  (const int32_t*)(app ? packed(a[8], I32, {n}, dev, "suffix_len") : nullptr), (float*)packed(a[12], F32, {n, Hkv, cap}, dev, "own_weight"),
+                  (int32_t*)packed(a[13], I32, {n, Hkv, cap}, dev, "own_position"), (int32_t*)(app ? packed(a[9], I32, {1}, dev, "status") : nullptr),
                   c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream());
   });
 }

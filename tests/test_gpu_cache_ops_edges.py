@@ -150,3 +150,17 @@ def test_readme_example_runs(mb):  # noqa: F811
     newest = sorted(range(P + budget + 5))[-recent:]
     for row in e["position"][:, :, :budget].reshape(-1, budget).tolist():
         assert len(set(row)) == budget and set(newest) <= set(row)
+
+
+def test_rotate_only_ignores_lengths_and_status(mb):  # noqa: F811
+    """q alone, with the lengths (of fewer streams than rows) and the status of the call that appends left in place"""
+    n, T, Hq, hd = 2, 5, 4, 64
+    g = torch.Generator(device="cuda").manual_seed(0)
+    q = torch.randn(n * T, Hq, hd, generator=g, device="cuda", dtype=torch.float16)
+    pos, freq, st = i32(np.arange(n * T)), mb.mlora_rope_frequencies(hd, 1e4)[0].cuda(), status()
+    a, b = torch.empty_like(q), torch.empty_like(q)
+    mb.mlora_rope_append(q, None, None, pos, freq, a, None, None, None, None)
+    mb.mlora_rope_append(q, None, None, pos, freq, b, None, None, i32([99, -7]), st)
+    assert torch.equal(a, b) and int(st.item()) == 0
+    with pytest.raises(mb.MloraError):             # totals and positions belong to appended rows
+        mb.mlora_rope_append(q, None, None, pos, freq, b, None, None, None, None, own_weight=torch.zeros(n, 2, 8, device="cuda"))
