@@ -1,5 +1,7 @@
 """Builds libmlora.so (sm_100a only) next to this file with nvcc, and with the host compiler the module that checks and hands on the
 tensors of its cache operators.  No JIT cache: both stay in-tree."""
+import importlib.metadata
+import importlib.util
 import os
 import subprocess
 import sys
@@ -36,16 +38,6 @@ def build(force=False, verbose=False):
             continue
         cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", src, "-o", obj]
         procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    marshal_src = os.path.join(CSRC, "marshal.cpp")
-    if force or not _newer(MARSHAL, [marshal_src, headers[-1]]):
-        import torch
-        root = os.path.dirname(torch.__file__)
-        inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
-               os.path.join(os.path.dirname(os.path.dirname(nvcc)), "include")]
-        lib = os.path.join(root, "lib")
-        cmd = ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
-               ["-isystem" + d for d in inc] + [marshal_src, "-o", MARSHAL, "-L" + lib, "-Wl,-rpath," + lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
-        procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for cmd, p in procs:
         out, _ = p.communicate()
         if verbose or p.returncode:
@@ -55,7 +47,48 @@ def build(force=False, verbose=False):
     if force or procs or not _newer(LIB, objs):
         cmd = [nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", LIB] + objs + ["-lcudart"]
         subprocess.check_call(cmd)
+    build_marshal(force, verbose)
     return LIB
+
+
+def _marshal_made_for():
+    """The torch and Python that `_marshal.so` is compiled against; None where there is no torch"""
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        return None
+    return f"{spec.origin} {importlib.metadata.version('torch')} {sys.implementation.cache_tag}\n"
+
+
+def build_marshal(force=False, verbose=False):
+    """The module that hands on the tensors of the cache operators, after the library, which does not need it.  Made again when its
+    sources, torch or Python change; left out where there is no torch (then nothing can import the binding either)."""
+    made_for = _marshal_made_for()
+    if made_for is None:
+        return
+    src, stamp = os.path.join(CSRC, "marshal.cpp"), MARSHAL + ".made_for"
+    if not force and _newer(MARSHAL, [src, os.path.join(HERE, "..", "include", "mlora.h")]) and os.path.exists(stamp):
+        with open(stamp) as f:
+            if f.read() == made_for:
+                return
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
+           os.path.join(cuda, "include")]
+    lib = os.path.join(root, "lib")
+    cmd = ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
+           ["-isystem" + d for d in inc] + [src, "-o", MARSHAL, "-L" + lib, "-Wl,-rpath," + lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+    try:
+        done = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        out, code = done.stdout, done.returncode
+    except OSError as e:
+        out, code = f"{e}\n", 1
+    if verbose or code:
+        sys.stderr.write(out)
+    if code:
+        raise RuntimeError("libmlora.so is built, _marshal.so (the binding's calls around a bounded KV cache) is not: " + " ".join(cmd))
+    with open(stamp, "w") as f:
+        f.write(made_for)
 
 
 if __name__ == "__main__":
