@@ -3,8 +3,9 @@
 //
 // A pair (a, b) of a row at position p turns by the angle p * f:  a' = a c - b s,  b' = b c + a s,  c = gain cos, s = gain sin.
 // Pairs are (i, i + rotary/2) or (2i, 2i + 1), i < rotary/2; features from `rotary` on pass through; v passes through.
-// Angles: p * f / 2 pi in 64 bits, its fraction of a turn (exact) rounded to 32 bits, sincospi of twice that: good to 2^-22
-// rad at any position (p = 10^6 in 32 bits would be off by 0.06 rad).
+// Angles: p * f / 2 pi in 64 bits with the products' rounding errors carried along, its fraction of a turn rounded to 32 bits, sincospi
+// of twice that: good to 2^-22 rad at any 32-bit position and frequencies up to 2^16 (p = 10^6 in 32 bits would be off by 0.06 rad; 64 bits
+// without the errors by 2^-21 at 2^31).
 // Bound by bytes: every feature is read and written once, 16 bytes at a time (83% of the copy rate for 16384 fp16 rows, 76% for 5003
 // fp32 rows).  A CTA first fills a table of its rows' cos and sin (one thread a pair, shared by all heads), the loads of its first
 // features being on their way meanwhile; 64 registers, so that four CTAs share an SM (with 100 and twice the reads in flight: 41 us).
@@ -40,6 +41,14 @@ template <> struct RopeVec<true> {
 __device__ __forceinline__ uint4 rope_pack(const float (&f)[8]) {
   return make_uint4(h2_as_u32(__floats2half2_rn(f[0], f[1])), h2_as_u32(__floats2half2_rn(f[2], f[3])),
                     h2_as_u32(__floats2half2_rn(f[4], f[5])), h2_as_u32(__floats2half2_rn(f[6], f[7])));
+}
+
+// The angle p f as half turns in [-1, 1]: 1 / 2 pi as a sum of two doubles, the errors of both products by fma
+__device__ __forceinline__ float rope_half_turns(double p, double f) {
+  constexpr double INV = 0.15915494309189533577, INV_REST = -9.8393383375912429e-18;
+  const double a = p * f, a_rest = fma(p, f, -a), t = a * INV;
+  const double rest = fma(a_rest, INV, fma(a, INV_REST, fma(a, INV, -t)));
+  return (float)(2.0 * ((t - rint(t)) + rest));
 }
 
 // An item is 16 features of a head: two pieces of 8 that hold the two halves of 8 pairs (half-split), or 16 neighbours.  Which 16 is
@@ -101,8 +110,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const RopeArg
   }
   for (int i = tid; i < in_rows * half; i += ROPE_THREADS) {
     const int x = ROWS == 1 ? 0 : i / half, j = i - x * half;
-    const double turns = (double)p.positions[row0 + x] * p.freq[j] * 0.15915494309189533577;
-    const float t = (float)(2.0 * (turns - rint(turns)));
+    const float t = rope_half_turns((double)p.positions[row0 + x], p.freq[j]);
     float sn, cn;
     sincospif(t, &sn, &cn);
     cs[x][j] = make_float2(cn * p.gain, sn * p.gain);

@@ -164,3 +164,26 @@ def test_rotate_only_ignores_lengths_and_status(mb):  # noqa: F811
     assert torch.equal(a, b) and int(st.item()) == 0
     with pytest.raises(mb.MloraError):             # totals and positions belong to appended rows
         mb.mlora_rope_append(q, None, None, pos, freq, b, None, None, None, None, own_weight=torch.zeros(n, 2, 8, device="cuda"))
+
+
+@pytest.mark.parametrize("pos", [2**31 - 1, -2**31, 2**31 - 12345, 2**30 + 77, -2**30 - 1, 1 << 24, -12345])
+def test_rope_angles_of_far_positions(mb, pos):  # noqa: F811
+    """Angles next to a quarter turn, so that the rotated 1 is a small number that fp16 resolves: off by 2^-22 at most (the angle), by half a
+    step of fp16 below 2^-13 (2^-25), and by the 1 in 2^24 that products and sums of 32 bits round by.  Reference in 64-bit mantissas."""
+    L, hd = np.longdouble, 128
+    if np.finfo(L).nmant < 63:
+        pytest.skip("long double is no longer than double here")
+    two_pi = L("6.283185307179586476925286766559005768")
+    rng = np.random.default_rng(pos % 1000)
+    k = rng.integers(int(abs(pos) * 0.5 / 6.2832), int(abs(pos) * 0.999 / 6.2832) + 1, hd // 2)
+    f = ((k + L("0.25") + L(2.0)**-17 * (rng.random(hd // 2) - 0.5)) * two_pi / abs(pos)).astype(np.float64)
+    angle = L(pos) * f.astype(L)
+    want = np.cos(angle).astype(np.float64)
+    assert (np.abs(want) < 2.0**-13).all() and (f < 1.01).all()
+    q = torch.zeros(1, 1, hd, device="cuda")
+    q[0, 0, :hd // 2] = 1.0
+    out = torch.empty(1, 1, hd, dtype=torch.float16, device="cuda")
+    mb.mlora_rope_append(q, None, None, i32([pos]), dev(f), out, None, None, None, None)
+    got = out[0, 0].double().cpu().numpy()
+    assert (np.abs(got[:hd // 2] - want) <= 2.0**-22 + 2.0**-25 + 2.0**-24 * np.abs(want)).all(), np.log2(np.abs(got[:hd // 2] - want).max())
+    assert (got[hd // 2:] == np.sign(np.sin(angle))).all()
