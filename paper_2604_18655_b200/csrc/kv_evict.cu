@@ -296,14 +296,13 @@ __global__ void __launch_bounds__(THREADS) kv_select_kernel(const EvictArgs p, c
     n_new = __reduce_add_sync(0xffffffffu, lane < ctas ? (int)ev_remote(&s_cta[0], lane) : 0);
   }
   const bool among_new = n_new >= B;
-  int want = among_new ? B : B - n_new;                    // rows of the class that stay (may be 0)
-  const bool none = want == 0;
+  int want = among_new ? B : B - n_new;                    // rows of the class that stay (at least one)
   auto of_class = [&] { return among_new ? fresh : there & ~fresh; };
   // ---- the bin of the want-th largest of the class, again within that bin, ...
-  bool all_equal_stay = none;                              // the rows at `lo` all stay: nothing to count among them
+  bool all_equal_stay = false;                             // the rows at `lo` all stay: nothing to count among them
   if (tid == 0) s_got[0] = s_got[1] = s_got[2] = 0;
   // (three rounds at most; the bound, and those on the list below, hold even if another stream writes the totals meanwhile)
-  for (int round = 0; round < 4 && !none && lo < hi; ++round) {
+  for (int round = 0; round < 4 && lo < hi; ++round) {
     const int shift = max(0, 32 - __clz(hi - lo) - 11);    // (hi - lo) >> shift < 2048
     pass([&] {
       const uint32_t cls = of_class();
@@ -389,11 +388,9 @@ __global__ void __launch_bounds__(THREADS) kv_select_kernel(const EvictArgs p, c
   auto stay_bits = [&] {                                   // (once a pass and chunk, in order)
     const uint32_t cls = of_class();
     uint32_t stay = 0u;
-    if (!none) {
 #pragma unroll
-      for (int j = 0; j < CH; ++j) stay |= (uint32_t)(key[j] >= lo) << j;
-      stay &= cls;
-    }
+    for (int j = 0; j < CH; ++j) stay |= (uint32_t)(key[j] >= lo) << j;
+    stay &= cls;
     if (!all_equal_stay) {
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
