@@ -60,6 +60,7 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
   const __half *kb, *vb;
   float* sc;
   bool own = false;
+  int32_t lone_parent = -1;
   if (item < p.n_prefix_chunks * p.rt_prefix) {
     slot = item / p.rt_prefix;
     v0 = (item - slot * p.rt_prefix) * 16; v1 = min(v0 + 16, R_all);
@@ -82,8 +83,8 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
     const size_t seg = ((size_t)s * p.Hkv + kh) * p.cap * HD;
     kb = p.own_k + seg; vb = p.own_v + seg;
     sc = p.sc_own; ld = p.ld_own;
-    // (a single row has no mask to make; what its parent says is checked all the same)
-    if (p.T == 1 && p.parent != nullptr && k1 > S && tid == 0 && p.parent[s] != -1) atomicCAS(p.status, 0, MLORA_ERR_ARG);
+    // (a single row has no mask to make; what its parent says is reported all the same, at the end: nothing waits for it)
+    if (p.T == 1 && p.parent != nullptr && k1 > S && tid == 0) lone_parent = p.parent[s];
     if (p.T > 1 && k1 > S && tid < 16) {                   // ancestor-or-self masks of the tile's nodes
       unsigned long long mask = 0ull;
       if (v0 + tid < v1) {
@@ -312,6 +313,7 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
     *reinterpret_cast<float4*>(p.part_o + at * HD + c) = a;
     if (c == 0) *reinterpret_cast<float2*>(p.part_ml + at * 2) = make_float2(M, L);
   }
+  if (lone_parent != -1) atomicCAS(p.status, 0, MLORA_ERR_ARG);
 }
 
 constexpr int FIN_THREADS = 128, FIN_WARPS = FIN_THREADS / 32, FIN_KEYS = 128;   // keys of a warp, four a lane
