@@ -2020,17 +2020,18 @@ static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return na != 0 && nb != 0 && x < y + nb && y < x + na;
 }
 
-struct Span { const void* at; size_t bytes; };             // null: not given
-// does anything written meet anything read, or anything else written
+struct Span {                                              // addresses lo .. hi - 1; null or empty: none
+  uintptr_t lo, hi;
+  Span(const void* at, size_t bytes) : lo(at && bytes ? (uintptr_t)at : 0), hi(at && bytes ? (uintptr_t)at + bytes : 0) {}
+};
+// does anything written meet anything read, or anything else written (some forty comparisons: no branches)
 static bool outputs_meet(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  unsigned met = 0;
   for (const Span* o = outs.begin(); o != outs.end(); ++o) {
-    if (o->at == nullptr) continue;
-    for (const Span& i : ins)
-      if (i.at != nullptr && overlap(o->at, o->bytes, i.at, i.bytes)) return true;
-    for (const Span* x = outs.begin(); x != o; ++x)
-      if (x->at != nullptr && overlap(o->at, o->bytes, x->at, x->bytes)) return true;
+    for (const Span& i : ins) met |= (o->lo < i.hi) & (i.lo < o->hi);
+    for (const Span* x = outs.begin(); x != o; ++x) met |= (o->lo < x->hi) & (x->lo < o->hi);
   }
-  return false;
+  return met != 0;
 }
 
 int mlora_rope_append(const void* q, const void* k, const void* v, int32_t in_fp32, int64_t q_stride, int64_t k_stride,
@@ -2058,8 +2059,8 @@ int mlora_rope_append(const void* q, const void* k, const void* v, int32_t in_fp
   if (q && q == q_out && (in_fp32 || q_stride != (int64_t)Hq * hd)) return fail(MLORA_ERR_ARG, "rope_append: in place only for packed fp16 rows");
   // (another CTA may still have to read what this one would overwrite)
   const size_t rows = (size_t)n * T, q_row = (size_t)Hq * hd, kv_row = (size_t)Hkv * hd, size = in_fp32 ? 4 : 2, q_out_bytes = rows * q_row * 2;
-  const Span q_in{q == q_out ? nullptr : q, ((rows - 1) * (size_t)q_stride + q_row) * size};
-  if (q_in.at && overlap(q_in.at, q_in.bytes, q_out, q_out_bytes)) return fail(MLORA_ERR_ARG, "rope_append: q_out overlaps q");
+  const Span q_in(q == q_out ? nullptr : q, ((rows - 1) * (size_t)q_stride + q_row) * size);
+  if (outputs_meet({{q_out, q_out_bytes}}, {q_in})) return fail(MLORA_ERR_ARG, "rope_append: q_out overlaps q");
   const size_t entries = (size_t)n * Hkv * own_capacity * 4, segments = entries / 2 * hd;
   if (outputs_meet({{q_out, q_out_bytes}, {own_k, segments}, {own_v, segments}, {own_weight, entries}, {own_position, entries}},
                    {q_in, {k, ((rows - 1) * (size_t)k_stride + kv_row) * size}, {v, ((rows - 1) * (size_t)v_stride + kv_row) * size},
