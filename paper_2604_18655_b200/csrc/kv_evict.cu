@@ -88,7 +88,8 @@ __device__ __forceinline__ int4 ev_remote4(const void* own, int rank) {
 }
 
 // KPT: rows a thread holds in registers (0: any number, read again each time).  CL: the CTAs of a cluster share the segment.  Warp w of
-// CTA c has the rows from (c * WARPS + w) * 32 * KPT on (KPT = 0: an even share), lane l every 32nd of them.
+// CTA c has the rows from (c * WARPS + w) * 32 * KPT on (KPT = 0: an even share), lane l every 32nd of them.  FEW: at most EV_FEW rows are
+// too many, which the CTA always moves itself (no list in global memory).
 template <int THREADS, int KPT, bool CL, bool FEW>
 __global__ void __launch_bounds__(THREADS) kv_select_kernel(const EvictArgs p, const int move_here) {
   constexpr int WARPS = THREADS / 32, PER = EV_BINS / THREADS;
@@ -118,12 +119,12 @@ __global__ void __launch_bounds__(THREADS) kv_select_kernel(const EvictArgs p, c
     if (tid == 0 && blockIdx.x == 0) atomicCAS(p.status, 0, MLORA_ERR_ARG);
     S = S < 0 ? 0 : p.bound;
   }
-  if (!move_here) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (kv_move_kernel, which waits for this one)
+  if (!FEW && !move_here) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (kv_move_kernel, which waits for this one)
   const int B = p.budget;
   if (tid == 0 && blockIdx.x == 0) p.out_len[s] = min(S, B);
   int2* const list = p.moves + (size_t)pair * p.max_moves;
   if (S <= B) {                                            // nothing to drop
-    if (tid == 0 && rank == 0) p.counts[pair] = 0;
+    if (!FEW && tid == 0 && rank == 0) p.counts[pair] = 0;
     for (int i = rank * THREADS + tid; i < S; i += ctas * THREADS) {
       if (p.out_weight != p.weight) p.out_weight[base + i] = w[i];
       if (pos != nullptr && p.out_position != p.position) p.out_position[base + i] = pos[i];
@@ -262,15 +263,10 @@ __global__ void __launch_bounds__(THREADS) kv_select_kernel(const EvictArgs p, c
         s_few_list[n_moves++] = make_int2(m++, place);
       }
       s_few_moves = n_moves;
-      p.counts[pair] = n_moves;
-      if (!move_here)
-        for (int i = 0; i < n_moves && i < p.max_moves; ++i) list[i] = s_few_list[i];
     }
     __syncthreads();
-    if (move_here) {
-      if (p.hd == 64) ev_move<64, 1>(p, s_few_list, s_few_moves, pair, tid / 16, THREADS / 16, tid % 16);
-      else ev_move<128, 1>(p, s_few_list, s_few_moves, pair, tid / 32, THREADS / 32, tid % 32);
-    }
+    if (p.hd == 64) ev_move<64, 1>(p, s_few_list, s_few_moves, pair, tid / 16, THREADS / 16, tid % 16);
+    else ev_move<128, 1>(p, s_few_list, s_few_moves, pair, tid / 32, THREADS / 32, tid % 32);
   } else {
   // ---- the class in which the order is decided: the new rows where they alone fill the budget, else the others
   // -- and the range of all images, in which the histograms start.  One exchange for both.
@@ -481,7 +477,7 @@ cudaError_t launch_kv_evict(const EvictArgs& args, cudaStream_t st) {
   else if (a.bound <= 16384) e = ev_select<1024, 16, false>(a, 1, move_here, st);
   else if (a.bound <= 131072) e = ev_select<1024, 16, true>(a, a.bound <= 32768 ? 2 : (a.bound <= 65536 ? 4 : 8), move_here, st);
   else e = ev_select<1024, 0, true>(a, 8, move_here, st);
-  if (e != cudaSuccess || move_here) return e;
+  if (e != cudaSuccess || move_here) return e;             // (always so for the FEW kernels: max_moves is at most EV_FEW)
   cudaLaunchConfig_t cfg{};
   const int per = 4 * (256 / (a.hd / 4)), most = (a.max_moves + per - 1) / per;
   // (as many CTAs as fit, 32 segments 8192 -> 4096 rows 15.4 and 16.8 us by twice as many; twice as many past L2, 64 segments 16384 ->
