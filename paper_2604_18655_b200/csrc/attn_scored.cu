@@ -821,7 +821,7 @@ static cudaError_t sw_launch(const ScoredArgs& a, cudaStream_t st) {
   t.q = a.q; t.prefix_k = a.prefix_k; t.prefix_v = a.prefix_v; t.prefix_head_stride = (size_t)a.P * HD;
   t.own_k = a.own_k; t.own_v = a.own_v; t.own_head_stride = (size_t)a.cap * HD; t.own_stream_stride = t.own_head_stride * a.Hkv;
   // (its CTAs start while the masks are made)
-  t.pdl = 1; t.anc_late = 1; t.len_limit = a.suffix_bound + 1; t.suffix_len = a.suffix_len; t.anc = a.anc; t.depth = a.depth; t.out = a.out; t.status = a.status; t.part_o = a.part_o; t.part_ml = a.part_ml;
+  t.pdl = 1; t.anc_late = 1; t.len_limit = a.suffix_bound + 1; t.suffix_len = a.suffix_len; t.anc = a.anc; t.out = a.out; t.status = a.status; t.part_o = a.part_o; t.part_ml = a.part_ml;
   if ((e = launch_attention(t, st)) != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2];
@@ -986,8 +986,8 @@ void scored_plan(ScoredArgs& a, int sm_count) {
   sw_chunks(a, sm_count);
 }
 
-// tcgen05 form, behind the partial results: the rows' normalisers, masks (two floats a node) and depths
-static size_t sw_floats(const ScoredArgs& a, size_t slots) { return sc_rows(a) * slots * (a.hd + 2) + sc_rows(a) * 2 + ((size_t)a.n * a.T + 1) * 4; }
+// tcgen05 form, behind the partial results: the rows' normalisers and masks (two floats a node), on 16-byte boundaries
+static size_t sw_floats(const ScoredArgs& a, size_t slots) { return sc_rows(a) * slots * (a.hd + 2) + 4 + sc_rows(a) * 2 + (size_t)a.n * a.T * 2; }
 static size_t sc_floats(const ScoredArgs& a) {
   return sc_rows(a) * ((size_t)(a.n_prefix_chunks + a.n_own_chunks) * (a.hd + 2) + (size_t)a.ld_prefix + a.ld_own);
 }
@@ -1029,7 +1029,6 @@ void scored_carve(ScoredArgs& a, float* ws) {              // ws: 16-byte aligne
     float* const at = a.part_ml + (parts * 2 + 3) / 4 * 4;
     a.row_ml = (float2*)at;
     a.anc = (unsigned long long*)(a.row_ml + sc_rows(a));
-    a.depth = (int32_t*)(a.anc + (size_t)a.n * a.T);
     return;
   }
   const size_t parts = sc_rows(a) * ((size_t)a.n_prefix_chunks + a.n_own_chunks);

@@ -37,8 +37,7 @@ struct ScoredArgs {
   int tc;                               // many rows a KV head: the tcgen05 kernels
   AttnArgs attn;                        // ... their attention
   float2* row_ml;                       // ... scratch: the rows' (maximum, 1 / sum)
-  unsigned long long* anc;              // ... scratch: ancestor masks, depths (not read)
-  int32_t* depth;
+  unsigned long long* anc;              // ... scratch: ancestor masks
 };
 cudaError_t init_scored();              // per device, once
 void scored_plan(ScoredArgs& a, int sm_count);
