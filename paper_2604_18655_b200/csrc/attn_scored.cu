@@ -27,6 +27,23 @@ __device__ __forceinline__ float sc_ex2(float x) {
   return y;
 }
 
+// The ancestor-or-self mask of node c of stream s.  A parent that is not an earlier node counts as the root and is reported, as is a root
+// that has one.
+__device__ __forceinline__ unsigned long long sc_ancestors(const ScoredArgs& p, int s, int c) {
+  if (p.parent == nullptr) return c >= 63 ? ~0ull : (1ull << (c + 1)) - 1;
+  const int32_t* par = p.parent + (size_t)s * p.T;
+  unsigned long long mask = 1ull;
+  bool bad = par[0] != -1;
+  for (int it = 0; it < 64 && c > 0; ++it) {
+    mask |= 1ull << c;
+    int pc = par[c];
+    if (pc < 0 || pc >= c) { bad = true; pc = 0; }
+    c = pc;
+  }
+  if (bad) atomicCAS(p.status, 0, MLORA_ERR_ARG);
+  return mask;
+}
+
 // One CTA: 16 query rows of a kv head against a chunk of keys, the warps taking 32 keys (16 of 128 features) in turn, each through a ring of its own
 // in shared memory that it fills with 16-byte asynchronous copies (keys past the end as zeros): STAGES - 1 steps ahead, and no warp
 // waits for another before the end.  The pieces of a row lie as with the 128-byte swizzle: piece i of key k at i ^ (k mod 8).
@@ -86,24 +103,7 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
     // (a single row has no mask to make; what its parent says is reported all the same, at the end: nothing waits for it)
     if (p.T == 1 && p.parent != nullptr && k1 > S && tid == 0) lone_parent = p.parent[s];
     if (p.T > 1 && k1 > S && tid < 16) {                   // ancestor-or-self masks of the tile's nodes
-      unsigned long long mask = 0ull;
-      if (v0 + tid < v1) {
-        int c = (v0 + tid) / G - s * p.T;
-        if (p.parent == nullptr) mask = c >= 63 ? ~0ull : (1ull << (c + 1)) - 1;
-        else {
-          const int32_t* par = p.parent + (size_t)s * p.T;
-          bool bad = par[0] != -1;
-          for (int it = 0; it < 64 && c > 0; ++it) {
-            mask |= 1ull << c;
-            int pc = par[c];
-            if (pc < 0 || pc >= c) { bad = true; pc = 0; }
-            c = pc;
-          }
-          mask |= 1ull;
-          if (bad) atomicCAS(p.status, 0, MLORA_ERR_ARG);
-        }
-      }
-      anc_s[tid] = mask;
+      anc_s[tid] = v0 + tid < v1 ? sc_ancestors(p, s, (v0 + tid) / G - s * p.T) : 0ull;
     }
     if (p.T > 1 && k1 > S) __syncthreads();
   }
@@ -783,8 +783,7 @@ scored_weights_kernel(const __grid_constant__ ScoredArgs p, const int rb, const 
   if (warp == 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
 }
 
-// What the tcgen05 kernels read of the pass: every node's ancestor-or-self mask (a malformed parent counts as the root).  Reports that and
-// lengths out of their bound.
+// What the tcgen05 kernels read of the pass: every node's ancestor-or-self mask.  Reports malformed parents and lengths out of their bound.
 __global__ void scored_prep_kernel(const ScoredArgs p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // (the attention kernel, which waits for this one)
   const int i = blockIdx.x * blockDim.x + threadIdx.x;
@@ -794,21 +793,7 @@ __global__ void scored_prep_kernel(const ScoredArgs p) {
   }
   if (i >= p.n * p.T) return;
   const int s = i / p.T;
-  int c = i - s * p.T;
-  unsigned long long mask = 1ull;
-  if (p.parent == nullptr) mask = c >= 63 ? ~0ull : (1ull << (c + 1)) - 1;
-  else {
-    const int32_t* par = p.parent + (size_t)s * p.T;
-    bool bad = par[0] != -1;
-    for (int it = 0; it < 64 && c > 0; ++it) {
-      mask |= 1ull << c;
-      int pc = par[c];
-      if (pc < 0 || pc >= c) { bad = true; pc = 0; }
-      c = pc;
-    }
-    if (bad) atomicCAS(p.status, 0, MLORA_ERR_ARG);
-  }
-  p.anc[i] = mask;
+  p.anc[i] = sc_ancestors(p, s, i - s * p.T);
 }
 
 template <int HD>
