@@ -1,5 +1,5 @@
-"""Calls around a bounded KV cache whose tensors lie over each other: refused on the host, each by the check that is meant.  The base
-arguments of every call are apart, so that one change is one fault.  No GPU."""
+"""Refusals of the calls around a bounded KV cache, each by the check that is meant: tensors that lie over each other, and the rest.  The
+base arguments of every call are apart, so that one change is one fault.  No GPU."""
 import pytest
 
 ARG = -1
@@ -76,3 +76,64 @@ IN_PLACE = dict(out_weight=A[2], out_position=A[3])
     {**IN_PLACE, "out_len": A[2]}, {**IN_PLACE, "out_source": A[3]}, {**IN_PLACE, "own_v": A[3]}, dict(out_weight=A[3], out_position=A[2])])
 def test_kv_evict_refuses_outputs_over_what_it_reads(mb, change):
     assert "overlap" in refused(mb, "mlora_kv_evict", EVICT, change)
+
+
+# ------------------------------------------------------------------ the other refusals, each by its own check
+UNSUPPORTED, CAPACITY = -6, -3
+
+
+def each(fragment, *changes, code=ARG):
+    return [pytest.param(code, fragment, c, id=f"{fragment}-{'-'.join(f'{k}={v}' for k, v in c.items())}".replace(" ", "_")) for c in changes]
+
+
+def by_its_own_check(mb, name, good, code, fragment, change):
+    assert set(change) <= set(good)
+    assert getattr(mb.lib(), name)(*{**good, **change}.values()) == code
+    assert fragment in mb.lib().mlora_last_error(None).decode()
+
+
+NO_KV = dict(k=None, v=None, own_k=None, own_v=None)
+
+
+@pytest.mark.parametrize("code,fragment,change", [
+    *each("null argument", dict(positions=None), dict(freq=None)),
+    *each("q and q_out go together", dict(q=None), dict(q_out=None)),
+    *each("k, v, own_k and own_v go together", dict(k=None), dict(v=None), dict(own_k=None), dict(own_v=None)),
+    *each("nothing to do", dict(q=None, q_out=None, **NO_KV)),
+    *each("null suffix_len or status", dict(suffix_len=None), dict(status=None)),
+    *each("belong to appended rows", dict(own_position=None, **NO_KV), dict(own_weight=None, **NO_KV)),
+    *each("bad shape", dict(n=0), dict(n=-1), dict(T=0), dict(Hq=0), dict(Hkv=0), dict(Hkv=-2), dict(Hq=1 << 14), dict(n=1 << 20, T=1 << 20, cap=1 << 21)),
+    *each("head_dim", dict(hd=80), dict(hd=256), dict(hd=0), code=UNSUPPORTED),
+    *each("rotary_dim", dict(rotary_dim=0), dict(rotary_dim=24), dict(rotary_dim=80), dict(rotary_dim=-16), code=UNSUPPORTED),
+    *each("exceeds own_capacity", dict(cap=2), dict(cap=0), dict(cap=-1), code=CAPACITY),
+    *each("row strides", dict(q_stride=504), dict(q_stride=516), dict(q_stride=-512), dict(k_stride=132), dict(k_stride=120), dict(v_stride=0), dict(in_fp32=1, v_stride=130)),
+    *each("aligned", *[{k: ROPE[k] + 8} for k in ("q", "k", "v", "q_out", "own_k", "own_v")]),
+    *each("in place only", dict(q_out=A[0], in_fp32=1), dict(q_out=A[0], q_stride=1024))])
+def test_rope_append_refuses_by_the_check_that_is_meant(mb, code, fragment, change):
+    by_its_own_check(mb, "mlora_rope_append", ROPE, code, fragment, change)
+
+
+@pytest.mark.parametrize("code,fragment,change", [
+    *each("null argument", *[{k: None} for k in ("q", "own_k", "own_v", "suffix_len", "out", "own_weight", "workspace", "status")]),
+    *each("null prefix", dict(prefix_k=None), dict(prefix_v=None)),
+    *each("bad shape", dict(n=0), dict(n=-1), dict(T=0), dict(T=65, cap=200), dict(Hq=7), dict(Hq=0), dict(Hkv=0), dict(Hkv=-2), dict(P=-1), dict(suffix_bound=-1),
+          dict(P=1 << 28), dict(suffix_bound=1 << 28, cap=(1 << 28) + 3), dict(Hq=1 << 17, Hkv=1 << 17), dict(n=1 << 27)),
+    *each("head_dim", dict(hd=96), dict(hd=256), code=UNSUPPORTED),
+    *each("exceeds own_capacity", dict(suffix_bound=62), dict(cap=42), dict(cap=-1), code=CAPACITY),
+    *each("workspace too small", dict(workspace_bytes=0), dict(workspace_bytes=64), code=CAPACITY),
+    *each("aligned", *[{k: SCORED[k] + 8} for k in ("q", "prefix_k", "prefix_v", "own_k", "own_v", "out")])])
+def test_attention_scored_refuses_by_the_check_that_is_meant(mb, code, fragment, change):
+    by_its_own_check(mb, "mlora_attention_scored", SCORED, code, fragment, change)
+
+
+@pytest.mark.parametrize("code,fragment,change", [
+    *each("null argument", *[{k: None} for k in ("own_k", "own_v", "own_weight", "suffix_len", "out_weight", "out_len", "workspace", "status")]),
+    *each("go together", dict(own_position=None), dict(out_position=None)),
+    *each("bad shape", dict(n=0), dict(n=-1), dict(Hkv=0), dict(n=40000), dict(suffix_bound=-1), dict(budget=0), dict(budget=-3)),
+    *each("recent needs", dict(newest=None), dict(own_position=None, out_position=None), dict(recent=33), dict(recent=-1)),
+    *each("head_dim", dict(hd=32), dict(hd=96), code=UNSUPPORTED),
+    *each("exceeds own_capacity", dict(suffix_bound=65), dict(cap=39), code=CAPACITY),
+    *each("workspace too small", dict(workspace_bytes=0), dict(workspace_bytes=64), code=CAPACITY),
+    *each("aligned", dict(own_k=A[0] + 8), dict(own_v=A[1] + 2))])
+def test_kv_evict_refuses_by_the_check_that_is_meant(mb, code, fragment, change):
+    by_its_own_check(mb, "mlora_kv_evict", EVICT, code, fragment, change)
