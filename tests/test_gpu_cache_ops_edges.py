@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from tests.test_gpu_cache_ops import dev, i32, mb, status  # noqa: F401
+from tests.test_gpu_cache_ops import Loop, close_fp16, dev, i32, mb, rotated, split, status  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -187,3 +187,72 @@ def test_rope_angles_of_far_positions(mb, pos):  # noqa: F811
     got = out[0, 0].double().cpu().numpy()
     assert (np.abs(got[:hd // 2] - want) <= 2.0**-22 + 2.0**-25 + 2.0**-24 * np.abs(want)).all(), np.log2(np.abs(got[:hd // 2] - want).max())
     assert (got[hd // 2:] == np.sign(np.sin(angle))).all()
+
+
+@pytest.mark.parametrize("n,Hq,Hkv,hd,P,B,recent", [(2, 8, 2, 64, 40, 16, 4), (3, 6, 3, 128, 0, 21, 1)])
+def test_every_step_of_a_bounded_stream_against_64_bits(mb, n, Hq, Hkv, hd, P, B, recent):  # noqa: F811
+    """INT4 projection -> rotate and append -> attention with totals -> eviction, until well past the budget.  Every step is computed in 64 bits
+    from what the GPU had before it (the projection's rows, cache, totals): rotated rows, output, totals, and which row goes."""
+    import gen
+    rng = np.random.default_rng(hd)
+    K, r, G, W, R = 256, 8, Hq // Hkv, (Hq + 2 * Hkv) * hd, hd
+    qb, sc = gen.quantize_int4(rng.standard_normal((K, W)).astype(np.float32) * 0.1, 64)
+    w = mb.mlora_weight_create(dev(qb), dev(sc), K, W, 64)
+    low = [dev(rng.standard_normal((r, K)).astype(np.float16)), dev((rng.standard_normal((r, W)) * 0.1).astype(np.float16))]
+    pA, pB = (torch.tensor([m.data_ptr()], dtype=torch.int64, device="cuda") for m in low)
+    scale, pick = torch.ones(1, device="cuda"), i32([0] * n)
+    lws = torch.zeros(mb.mlora_linear_workspace_bytes(w, n, r), dtype=torch.uint8, device="cuda")
+    lp, y = Loop(mb, n, 1, Hq, Hkv, hd, P, B, recent, seed=hd), torch.empty(n, W, device="cuda")
+    if not P:
+        lp.pk = lp.pv = lp.pw = None
+    freq, dropped = lp.freq.cpu().numpy(), 0
+    for i in range(B + 12):
+        mb.mlora_linear(w, dev(rng.standard_normal((n, K)).astype(np.float16)), y, lws, pick, pA, pB, scale, r)
+        S, pos = lp.lens.tolist(), lp.pos.cpu().numpy()
+        was = [t.clone() for t in (lp.k, lp.v, lp.w, lp.p)]
+        pw = lp.pw.double().clone() if P else None
+        lp.step(*split(y, Hq, Hkv, hd))
+        assert lp.lens.tolist() == [min(s + 1, B) for s in S] and int(lp.st.item()) == 0
+        x = y.double().cpu().numpy()
+        close_fp16(lp.q, *rotated(x[:, :Hq * hd].reshape(n, Hq, hd), pos, freq, 1.0, R, False))
+        new_k, size_k = rotated(x[:, Hq * hd:(Hq + Hkv) * hd].reshape(n, Hkv, hd), pos, freq, 1.0, R, False)
+        new_v = x[:, (Hq + Hkv) * hd:].astype(np.float16).reshape(n, Hkv, hd)
+        grown_p, grown_tol = (torch.zeros(Hkv, P, dtype=torch.float64, device="cuda"), 0.0) if P else (None, 0.0)
+        for s in range(n):
+            L = S[s] + 1
+            for h in range(Hkv):
+                src = lp.src[s, h, :min(L, B)].tolist()
+                place = src.index(S[s])            # (the new row stays: it is among the `recent` ones)
+                k, v, t, p = (a[s, h, :L].clone() for a in was)
+                k[S[s]], v[S[s]], t[S[s]], p[S[s]] = lp.k[s, h, place], lp.v[s, h, place], 0.0, int(pos[s])
+                close_fp16(k[S[s]], new_k[s, h], size_k[s, h])
+                assert np.array_equal(v[S[s]].cpu().numpy(), new_v[s, h])
+                ks, vs = (torch.cat([a[h], b]).double() for a, b in ((lp.pk, k), (lp.pv, v))) if P else (k.double(), v.double())
+                q = lp.q[s, h * G:(h + 1) * G].double()
+                pr = torch.softmax(q @ ks.T / np.sqrt(hd), dim=-1)
+                # a score: hd products added in 32 bits; a weight: scores' errors twice, 2^-20 for exponentials and sums; weights as fp16 for the
+                # product (2^-11, or 2^-25 of the largest below the normal range), the output as fp16
+                delta = float((q.abs() @ ks.abs().T).max()) / np.sqrt(hd) * (hd + 8) * 2.0**-23
+                want, size = pr @ vs, pr @ vs.abs()
+                tol = 2.0**-11 * want.abs() + (2.0**-11 + 2 * delta + 2.0**-20) * size * (1 + 2.0**-8) + 2.0**-25 * vs.abs().sum(dim=0) + 2.0**-25
+                assert bool(((lp.out[s, h * G:(h + 1) * G].double() - want).abs() <= tol).all()), (i, s, h)
+                rel = 2 * delta + 2.0**-20 + G * 2.0**-24
+                add = pr.sum(dim=0)
+                total = t.double() + add[P:]
+                # (an exponential below the smallest normal number of 32 bits, 2^-126 of the row's largest, counts as zero: so much is lost a row,
+                # a weight being an exponential divided by a sum of at least one)
+                total_tol = rel * add[P:] + 2.0**-23 * total + G * 2.0**-126
+                assert bool(((lp.w[s, h, :len(src)].double() - total[src]).abs() <= total_tol[src]).all()), (i, s, h)
+                assert torch.equal(lp.p[s, h, :len(src)], p[src]) and torch.equal(lp.k[s, h, :len(src)], k[src]) and torch.equal(lp.v[s, h, :len(src)], v[src])
+                if P:
+                    grown_p[h] += add[:P]
+                    grown_tol = max(grown_tol, rel)
+                if L > B:                          # the smallest total of the rows that are not new, but for what the totals round by
+                    (gone,) = set(range(L)) - set(src)
+                    old = p <= int(pos[s]) - recent
+                    assert bool(old[gone]) and float(total[gone] - total_tol[gone]) <= float((total + total_tol)[old].min())
+                    dropped += 1
+        if P:
+            assert bool(((lp.pw.double() - pw - grown_p).abs() <= (grown_tol + n * G * 2.0**-24) * grown_p + 2.0**-23 * (pw + grown_p) + n * G * 2.0**-126).all())
+    mb.mlora_weight_destroy(w)
+    assert dropped == n * Hkv * 12
