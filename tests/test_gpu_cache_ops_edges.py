@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from tests.test_gpu_cache_ops import Loop, close_fp16, dev, i32, mb, rotated, split, status  # noqa: F401
+from tests.test_gpu_cache_ops import Loop, close_fp16, dev, evict_case, evict_reference, i32, mb, rotated, rows, split, status  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -256,3 +256,35 @@ def test_every_step_of_a_bounded_stream_against_64_bits(mb, n, Hq, Hkv, hd, P, B
             assert bool(((lp.pw.double() - pw - grown_p).abs() <= (grown_tol + n * G * 2.0**-24) * grown_p + 2.0**-23 * (pw + grown_p) + n * G * 2.0**-126).all())
     mb.mlora_weight_destroy(w)
     assert dropped == n * Hkv * 12
+
+
+@pytest.mark.parametrize("T", [1, 20])
+def test_nan_totals_go_from_the_attention_into_the_eviction(mb, T):  # noqa: F811
+    """A cached key of NaN: its stream's outputs and totals become NaN, and eviction keeps the new rows and then the first ones; the other
+    streams come out with the bits that they have without it"""
+    n, Hq, Hkv, hd, P, B, recent = 3, 8, 2, 64, 70, 60, 25
+    xs = rows(3, 3, n, T, (Hq + 2 * Hkv) * hd)
+    ref, lp = (Loop(mb, n, T, Hq, Hkv, hd, P, B, recent, seed=4, kept=B - 3) for _ in range(2))
+    lp.k[1, 0, 0, 5] = float("nan")
+    for x in xs:
+        ref.step(*split(x, Hq, Hkv, hd))
+        before_p, S = lp.p.cpu().numpy(), lp.lens.tolist()[1]
+        before_p[1, 0, S:S + T] = lp.pos.view(n, T)[1].cpu().numpy()
+        lp.step(*split(x, Hq, Hkv, hd))
+        newest = int(lp.newest[1])
+        want = evict_reference(np.full(S + T, np.nan, dtype=np.float32), before_p[1, 0], S + T, B, recent, newest)
+        assert lp.src[1, 0, :len(want)].tolist() == want.tolist()
+        assert bool(lp.w[1, 0, :min(S + T, B)].isnan().all()) and bool(lp.out.view(n, T, Hq, hd)[1, :, :Hq // Hkv].isnan().all())
+    assert int(lp.st.item()) == 0 and bool(lp.pw[0].isnan().all())
+    keep = [0, 2]
+    for a, b in zip((lp.out.view(n, -1), lp.k, lp.v, lp.w, lp.p, lp.src), (ref.out.view(n, -1), ref.k, ref.v, ref.w, ref.p, ref.src)):
+        assert torch.equal(a[keep], b[keep])
+    assert torch.equal(lp.w[1, 1], ref.w[1, 1]) and torch.equal(lp.src[1, 1], ref.src[1, 1]) and torch.equal(lp.pw[1], ref.pw[1])
+
+
+@pytest.mark.parametrize("n,Hkv,hd,S,B", [(8, 8, 64, 16384, 8192), (16, 8, 128, 8192, 4096)])
+def test_evict_more_than_l2_holds(mb, n, Hkv, hd, S, B):  # noqa: F811
+    """Moves of over 100 MB: what is read is marked to leave L2 first too, the moving kernel (64 segments) has twice the blocks; and 128
+    segments, moved by the selecting blocks"""
+    assert n * Hkv * B * hd * 4 > 100000000
+    evict_case(mb, n, Hkv, hd, [S - 331 * (s % 5) for s in range(n)], B, 100, seed=n, in_place=n == 8)
