@@ -297,8 +297,9 @@ __global__ void __launch_bounds__(THREADS) kv_select_kernel(const EvictArgs p, c
   // ---- the bin of the want-th largest of the class, again within that bin, ...
   bool all_equal_stay = false;                             // the rows at `lo` all stay: nothing to count among them
   if (tid == 0) s_got[0] = s_got[1] = s_got[2] = 0;
-  // (three rounds at most; the bound, and those on the list below, hold even if another stream writes the totals meanwhile)
-  for (int round = 0; round < 4 && lo < hi; ++round) {
+  // (32 bits of range by 11 a round: three are enough; the bound, and those on the list below, hold even if another stream writes the
+  // totals meanwhile)
+  for (int round = 0; round < 3 && lo < hi; ++round) {
     const int shift = max(0, 32 - __clz(hi - lo) - 11);    // (hi - lo) >> shift < 2048
     pass([&] {
       const uint32_t cls = of_class();
