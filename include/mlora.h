@@ -326,10 +326,11 @@ int mlora_attention(const void* q, const void* prefix_k, const void* prefix_v, i
 
 /* ---- operators around a bounded KV cache (kernel-level) ----
  * What a program that drives the kernel-level calls itself needs between its projections and mlora_attention, and what lets a
- * stream run on when its own segment is full: rotate and append a pass's rows, attend while totalling what every cached key
- * contributes, drop the keys that contribute least.  own_weight and own_position lie beside the own segments, one entry for
- * every row of every KV head: float / int32 [n_streams][n_kv_heads][own_capacity].  The own segment is a set as far as
- * attention goes (a key's position is in its rotation), so rows may lie in any order.  head_dim 64 or 128; K, V, q and out
+ * stream of its own run on when its segment is full: rotate and append a pass's rows, attend while totalling what every cached
+ * key contributes, drop the keys that contribute least.  (A context's streams keep their caches to themselves: they end in
+ * MLORA_ERR_CAPACITY.)  own_weight and own_position lie beside the own segments, one entry for every row of every KV head: float
+ * / int32 [n_streams][n_kv_heads][own_capacity].  The own segment is a set as far as attention goes (a key's position is in its
+ * rotation), so rows may lie in any order.  head_dim 64 or 128; K, V, q and out
  * 16-byte aligned.  All pointers are of the current device.  Lengths that only the device sees and that are out of range set
  * the status word; the call then stays in bounds.  A workspace serves one call at a time. */
 
@@ -337,8 +338,9 @@ int mlora_attention(const void* q, const void* prefix_k, const void* prefix_v, i
  * (host) the factor on cos and sin.  PLAIN: f_i = theta^(-2 i / rotary_dim).  For contexts longer than a model was trained on
  * (factor >= 1 times `length` positions): LINEAR: f_i / factor.  BASE: theta * factor^(d / (d - 2)).  WAVES: pairs that turn
  * at most `low` times in `length` positions are divided by factor, those that turn `high` times and more stay, a linear blend by
- * turns between.  RAMP ("YaRN"): the same two ends, a linear blend by pair index between them (floor / ceil of the pairs that
- * turn `high` / `low` times), gain 0.1 ln(factor) + 1.  Unused arguments are ignored.  Host only.  Errors: ARG. */
+ * turns between (usual: low 1, high 4).  RAMP ("YaRN"): the same two ends (usual: 1 and 32), a linear blend by pair index between
+ * them (floor / ceil of the pairs that turn `high` / `low` times), gain 0.1 ln(factor) + 1.  Unused arguments are ignored.  Host
+ * only: mlora_rope_append reads frequencies on the device.  Errors: ARG. */
 enum { MLORA_ROPE_PLAIN = 0, MLORA_ROPE_LINEAR = 1, MLORA_ROPE_BASE = 2, MLORA_ROPE_WAVES = 3, MLORA_ROPE_RAMP = 4 };
 int mlora_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, double length, double low,
                            double high, double* freq, float* gain);
@@ -368,9 +370,11 @@ size_t mlora_attention_scored_workspace_bytes(int32_t n_streams, int32_t n_nodes
  * the stream's n_nodes rows and the query heads that share KV head h, of the weight they give row j of the own segment (cached
  * rows and the pass's own); prefix_weight dev fp32 [n_kv_heads][prefix_len] (NULL: not wanted) by the same sum over the rows of
  * all streams.  Entries of rows behind suffix_len + n_nodes are not touched.  tree_parent may be NULL: the pass's rows form a
- * chain.  n_nodes <= 64.  out, own_weight, prefix_weight and the workspace overlap neither each other nor what is read.  The rows
- * of a pass should be finite: a weight of zero times an infinite or NaN value is NaN.  Results do not depend on the order in which
- * the GPU runs the work.
+ * chain.  n_nodes <= 64 (a prompt of more rows has no call of its own: totals to cut it by can be those of its last rows, up to
+ * 64).  A row's scores, maximum, sum and totals are held in 32 bits; the weights are rounded to fp16 for their product with V, as
+ * in mlora_attention: up to 2^-11 of sum(weight |V|) in out, beside its own rounding; totals do not have it.  out, own_weight,
+ * prefix_weight and the workspace overlap neither each other nor what is read.  The rows of a pass should be finite: a weight of
+ * zero times an infinite or NaN value is NaN.  Results do not depend on the order in which the GPU runs the work.
  * Errors: ARG, UNSUPPORTED, CAPACITY (suffix_bound + n_nodes > own_capacity, workspace), CUDA; a malformed parent array or a
  * suffix_len outside 0..suffix_bound sets the device status to MLORA_ERR_ARG. */
 int mlora_attention_scored(const void* q, const void* prefix_k, const void* prefix_v, int32_t prefix_len,

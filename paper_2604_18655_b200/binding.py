@@ -375,7 +375,8 @@ ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "waves": 3, "ramp": 4}
 
 
 def mlora_rope_frequencies(rotary_dim, theta=1e4, scaling="plain", factor=1.0, length=0.0, low=1.0, high=32.0):
-    """(CPU float64 [rotary_dim / 2] radians per position of every pair, factor on cos and sin); needs no GPU"""
+    """(CPU float64 [rotary_dim / 2] radians per position of every pair, factor on cos and sin); needs no GPU.  mlora_rope_append reads the
+    frequencies on the device: freq.cuda().  `high` is the usual one of "ramp"; for "waves" it is 4."""
     freq = torch.empty(max(int(rotary_dim), 2) // 2, dtype=torch.float64)
     gain = C.c_float(0.0)
     _check(lib().mlora_rope_frequencies(rotary_dim, theta, ROPE_SCALING[scaling], factor, length, low, high,

@@ -51,7 +51,7 @@ __device__ __forceinline__ unsigned long long sc_ancestors(const ScoredArgs& p, 
 // order of its features, nor an output on the order of its columns, so both are dealt to suit them:
 //   S:  lane (g, t) holds, of key g, the pieces 2 t + j of each 64 features; a piece feeds two k-steps (q is dealt the same way)
 //   PV: lane (g, t) holds, of keys 2t, 2t + 1, 2t + 8, 2t + 9, piece g of each 64 features; column g of n-tile i is feature 8 g + i
-// Long segments are bound by the bytes of K and V (eight streams of 16384 rows of 8 heads of 128: 93% of the copy rate), short ones by the
+// Long segments are bound by the bytes of K and V (eight streams of 16384 rows of 8 heads of 128: 85 us, 95% of the copy rate), short ones by the
 // length of a step's chain: two products with their exponentials between them take 0.6 us whether a step has 16 keys or 32 (heads of 64,
 // eight ragged streams of up to 2048 rows: 14.3 us by 16, 12.3 by 32; at 128 features 32 keys leave an SM one CTA: 12.0 and 14.6 us for
 // 8 x 16 nodes).
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(SC_WARPS * 32, ScCfg<HD>::CTAS) scored_rows_ke
     for (int nt = 0; nt < C::KEYS / 8; ++nt) {
       const float e0 = sc_ex2(s[nt][0] - b_a), e1 = sc_ex2(s[nt][1] - b_a);
       l_a += e0 + e1;
-      pf[nt >> 1][(nt & 1) * 2] = h2_as_u32(__floats2half2_rn(e0, e1));   // (weights up to 1 as fp16: half a step of 2^-11 of each)
+      pf[nt >> 1][(nt & 1) * 2] = h2_as_u32(__floats2half2_rn(e0, e1));   // (weights up to 1 as fp16 for mma: off by 2^-11 of each at most, 2^-25 below 2^-14; l adds up the 32-bit ones)
     }
     if (high) {
       const float b_z = m_z == -INFINITY ? 0.f : m_z;
@@ -550,7 +550,9 @@ __global__ void __launch_bounds__(FIN_THREADS, 5) scored_finish_kernel(const Sco
 // or a stream's rows (where they are one block) against several tiles of its own keys.  Two accumulators: the next product is made
 // while this one's exponentials are.  Many blocks of rows of a prefix tile are shared by a cluster of two CTAs, the second of which hands its
 // sums to the first.
-// What bounds it: the exponentials, 8 clocks an SM for a row of a tile (16 a clock).
+// Its floor would be the exponentials, 8 clocks an SM for a row of a tile (16 a clock); it takes three times that: one warpgroup reads an
+// accumulator and makes its exponentials in turn, while the other accumulator waits for it (8 x 32 nodes of llama3b heads: exponential unit
+// 30% busy, issue 26%, tensor pipe 15%).
 constexpr int SW_KEYS = 128, SW_ROWS = 128, SW_THREADS = 160;
 template <int HD> struct SwCfg {
   static constexpr uint32_t TILE = SW_KEYS * HD * 2;

@@ -6,9 +6,10 @@
 // Angles: p * f / 2 pi in 64 bits with the products' rounding errors carried along, its fraction of a turn rounded to 32 bits, sincospi
 // of twice that: good to 2^-22 rad at any 32-bit position and frequencies up to 2^16 (p = 10^6 in 32 bits would be off by 0.06 rad; 64 bits
 // without the errors by 2^-21 at 2^31).
-// Bound by bytes: every feature is read and written once, 16 bytes at a time (83% of the copy rate for 16384 fp16 rows, 76% for 5003
-// fp32 rows).  A CTA first fills a table of its rows' cos and sin (one thread a pair, shared by all heads), the loads of its first
-// features being on their way meanwhile; 64 registers, so that four CTAs share an SM (with 100 and twice the reads in flight: 41 us).
+// Bound by bytes: every feature is read and written once, 16 bytes at a time (81% of the copy rate for 16384 fp16 rows, 76% for 5003
+// fp32 rows; in a graph 88% and 81%).  A CTA first fills a table of its rows' cos and sin (one thread a pair, shared by all heads), the loads
+// of its first features being on their way meanwhile.  fp16: 64 registers, so that four CTAs share an SM (16384 rows with 100 registers and
+// twice the reads in flight: 41 us); fp32: 76 to 80, three CTAs.
 #include "../../include/mlora.h"
 #include "cache_ops.cuh"
 
@@ -175,7 +176,7 @@ template <bool F32, int HD>
 static cudaError_t rope_launch(const RopeArgs& a, cudaStream_t st) {
   const int rows = a.n * a.T;
   // Few rows: a CTA each.  Many: as many as make a sector of totals (8 rows of fp16: 16384 rows of 48 heads of 64 in 37.2 us, 4 rows
-  // 39.8), or of the same bytes (4 rows of fp32: 5003 rows of 40 heads of 128 in 30.9 us, 8 rows 33.3).
+  // 39.8; 38.4 since angles carry their rounding errors), or of the same bytes (4 rows of fp32: 5003 rows of 40 heads of 128 in 30.9 us, 8 rows 33.3).
   constexpr int ROWS = F32 ? 4 : 8;
   if (rows < 148 * 8) rope_append_kernel<F32, HD, 1, 2><<<rows, ROPE_THREADS, 0, st>>>(a);
   else rope_append_kernel<F32, HD, ROWS, 2><<<(rows + ROWS - 1) / ROWS, ROPE_THREADS, 0, st>>>(a);
