@@ -56,7 +56,11 @@ def _marshal_made_for():
     spec = importlib.util.find_spec("torch")
     if spec is None:
         return None
-    return f"{spec.origin} {importlib.metadata.version('torch')} {sys.implementation.cache_tag}\n"
+    try:
+        version = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:        # a source tree on the path
+        version = str(os.path.getmtime(spec.origin))
+    return f"{spec.origin} {version} {sys.implementation.cache_tag}\n"
 
 
 def build_marshal(force=False, verbose=False):

@@ -45,3 +45,12 @@ def test_module_is_made_again_for_another_torch_or_python(build, monkeypatch):
     monkeypatch.setattr(build, "_newer", lambda target, deps: True)
     with pytest.raises(RuntimeError):
         build.build_marshal()
+
+
+def test_torch_without_a_distribution_is_known_by_its_files(build, monkeypatch):
+    def missing(name):
+        raise build.importlib.metadata.PackageNotFoundError(name)
+    known = build._marshal_made_for()
+    monkeypatch.setattr(build.importlib.metadata, "version", missing)
+    other = build._marshal_made_for()
+    assert other and other != known and other == build._marshal_made_for()
